@@ -1,4 +1,4 @@
-"""ctypes binding of libdsllm_ckpt.so: same names as the C ABI (include/ckpt.h, include/ckpt_proxy.h),
+"""ctypes binding of libdsllm_ckpt.so: same names as the C ABI (include/ckpt.h, include/ckpt_proxy.h, include/ckpt_train.h),
 argument marshalling only. There is no fallback: if the library has not been built, importing this
 module raises."""
 import ctypes as C
@@ -143,12 +143,54 @@ _SIGS = {
     "proxy_stream_create": (C.c_int, [C.POINTER(_vp)]),
     "proxy_stream_destroy": (C.c_int, [_vp]),
 }
-for _name, (_res, _args) in _SIGS.items():
+
+
+class ckpt_mx_matrix(C.Structure):
+    _fields_ = [("format", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p),
+                ("code_pitch", C.c_uint64), ("scales", C.c_void_p), ("scale_pitch", C.c_uint64)]
+
+
+class ckpt_optim_tensor(C.Structure):
+    _fields_ = [("numel", C.c_uint64), ("dev_grad", C.c_void_p), ("dev_param", C.c_void_p), ("dev_master", C.c_void_p), ("dev_m", C.c_void_p),
+                ("dev_v", C.c_void_p), ("dev_m_scale", C.c_void_p), ("dev_v_scale", C.c_void_p), ("weight_decay", C.c_double)]
+
+
+class ckpt_optim_config(C.Structure):
+    _fields_ = [("grad_dtype", C.c_int32), ("param_dtype", C.c_int32), ("state_bits", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ckpt_norm_result(C.Structure):
+    _fields_ = [("sum_squares", C.c_double), ("norm", C.c_float), ("scale", C.c_float), ("nonfinite", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ckpt_adamw_args(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_uint64), ("seed", C.c_uint64),
+                ("rounding", C.c_int32), ("reserved", C.c_int32), ("dev_norm", C.c_void_p)]
+
+
+CKPT_MXFP4, CKPT_MXFP8 = 1, 2
+CKPT_ROUND_NEAREST, CKPT_ROUND_STOCHASTIC, CKPT_ROUND_NONZERO = 0, 1, 2
+
+_i64, _mx = C.c_int64, C.POINTER(ckpt_mx_matrix)
+_TRAIN_SIGS = {      # include/ckpt_train.h
+    "ckpt_mx_layout": (C.c_int, [_i32, _i64, _i64, _mx]),
+    "ckpt_mx_quantize": (C.c_int, [_vp, _i32, _i64, _mx, _mx, _i32, _u64, _vp]),
+    "ckpt_mx_dequantize": (C.c_int, [_mx, _vp, _i32, _i64, _vp]),
+    "ckpt_mx_gemm_workspace": (C.c_int, [_i64, _i64, _i64, C.POINTER(_u64)]),
+    "ckpt_mx_gemm": (C.c_int, [_mx, _mx, _vp, _i32, _i64, _i32, _vp, _u64, _vp]),
+    "ckpt_optim_create": (C.c_int, [C.POINTER(ckpt_optim_tensor), C.c_size_t, C.POINTER(ckpt_optim_config), C.POINTER(_vp)]),
+    "ckpt_optim_destroy": (C.c_int, [_vp]),
+    "ckpt_optim_set_grads": (C.c_int, [_vp, C.POINTER(_vp), C.c_size_t, _vp]),
+    "ckpt_optim_grad_norm": (C.c_int, [_vp, C.c_double, C.c_double, _vp, _vp]),
+    "ckpt_optim_adamw_step": (C.c_int, [_vp, C.POINTER(ckpt_adamw_args), _vp]),
+}
+for _name, (_res, _args) in {**_SIGS, **_TRAIN_SIGS}.items():
     _fn = getattr(lib, _name)      # raises if the library does not export the symbol
     _fn.restype = _res
     _fn.argtypes = _args
 
 EXPORTED = tuple(_SIGS)
+EXPORTED_TRAIN = tuple(_TRAIN_SIGS)
 
 
 def _check(rc):
@@ -372,6 +414,77 @@ class Checkpointer:
         if self._h:
             h, self._h = self._h, None
             _check(lib.ckpt_destroy(h))
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def mx_matrix(fmt, rows, cols, codes, code_pitch, scales, scale_pitch):
+    """A ckpt_mx_matrix: device addresses of codes and scales, bytes from row to row of each."""
+    return ckpt_mx_matrix(fmt, 0, rows, cols, codes, code_pitch, scales, scale_pitch)
+
+
+def mx_layout(fmt, rows, cols):
+    """ckpt_mx_layout: (code_pitch, scale_pitch), the smallest ones."""
+    out = ckpt_mx_matrix()
+    _check(lib.ckpt_mx_layout(fmt, rows, cols, C.byref(out)))
+    return out.code_pitch, out.scale_pitch
+
+
+def mx_quantize(src, src_dtype, ld, by_row, by_col, stream, rounding=CKPT_ROUND_NEAREST, seed=0):
+    """ckpt_mx_quantize: by_row, by_col are ckpt_mx_matrix or None."""
+    _check(lib.ckpt_mx_quantize(src, src_dtype, ld, by_row, by_col, rounding, seed, stream))
+
+
+def mx_dequantize(src, dst, dst_dtype, ld, stream):
+    _check(lib.ckpt_mx_dequantize(src, dst, dst_dtype, ld, stream))
+
+
+def mx_gemm_workspace(m, n, k):
+    """ckpt_mx_gemm_workspace: bytes of workspace that a product of these sizes can use."""
+    out = _u64()
+    _check(lib.ckpt_mx_gemm_workspace(m, n, k, C.byref(out)))
+    return out.value
+
+
+def mx_gemm(a, b, c, c_dtype, ldc, stream, accumulate=False, workspace=None, workspace_bytes=0):
+    """ckpt_mx_gemm: C (+)= A B^T; a, b are ckpt_mx_matrix."""
+    _check(lib.ckpt_mx_gemm(a, b, c, c_dtype, ldc, accumulate, workspace, workspace_bytes, stream))
+
+
+class Optimizer:
+    """One ckpt_optim. tensors: iterable of dicts with the fields of ckpt_optim_tensor without the "dev_" prefix (numel and
+    grad; master, m, v and, as the configuration asks for them, param, m_scale and v_scale; weight_decay)."""
+
+    def __init__(self, tensors, grad_dtype=CKPT_BF16, param_dtype=CKPT_BF16, state_bits=32):
+        tensors = list(tensors)
+        arr = (ckpt_optim_tensor * max(1, len(tensors)))()
+        for k, t in enumerate(tensors):
+            for name, value in t.items():
+                setattr(arr[k], name if name in ("numel", "weight_decay") else "dev_" + name, value)
+        cfg = ckpt_optim_config(grad_dtype, param_dtype, state_bits, 0)
+        self._h = _vp()
+        _check(lib.ckpt_optim_create(arr, len(tensors), C.byref(cfg), C.byref(self._h)))
+
+    def set_grads(self, grads, stream):
+        grads = list(grads)
+        _check(lib.ckpt_optim_set_grads(self._h, (_vp * max(1, len(grads)))(*grads), len(grads), stream))
+
+    def grad_norm(self, out, stream, max_norm=0.0, grad_scale=1.0):
+        """out: device address of a ckpt_norm_result."""
+        _check(lib.ckpt_optim_grad_norm(self._h, max_norm, grad_scale, out, stream))
+
+    def step(self, stream, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, stochastic=False, norm=None):
+        """ckpt_optim_adamw_step; norm: device address of a ckpt_norm_result, or None."""
+        _check(lib.ckpt_optim_adamw_step(self._h, ckpt_adamw_args(lr, beta1, beta2, eps, step, seed, 1 if stochastic else 0, 0, norm), stream))
+
+    def destroy(self):
+        if self._h:
+            h, self._h = self._h, None
+            _check(lib.ckpt_optim_destroy(h))
 
     def __del__(self):
         try:

@@ -1,0 +1,378 @@
+// The update phase over a list of tensors (include/ckpt_train.h): the norm of all gradients and the AdamW step, a launch each.
+#include <math.h>
+
+#include <memory>
+#include <vector>
+
+#include "train_util.hpp"
+
+using namespace dsllm;
+
+namespace {
+
+struct TensorEntry {
+    const uint8_t *grad;
+    uint8_t *param;
+    float *master;
+    uint8_t *m, *v, *m_scale, *v_scale;
+    uint64_t numel;
+    uint64_t first_block;      // blocks of 32 of all tensors before it
+    double weight_decay;
+};
+
+// What one block works on: `count` elements of a tensor from element `first`, a multiple of 32, on.
+struct Span {
+    uint32_t tensor, count;
+    uint64_t first;
+};
+constexpr uint32_t kSpan = 4096, kNormBlocks = 2048;
+
+struct NormScratch {
+    double partial[kNormBlocks];
+    uint32_t arrived;
+};
+
+}  // namespace
+
+struct ckpt_optim {
+    int device = 0;
+    size_t n = 0;
+    uint32_t n_spans = 0;
+    ckpt_optim_config cfg{};
+    bool has_state = false;
+    TensorEntry *dev_tensors = nullptr;
+    Span *dev_spans = nullptr;
+    NormScratch *dev_scratch = nullptr;
+    std::vector<uint64_t> numels;
+};
+
+namespace {
+
+// ------------------------------------------------------------------ gradient norm
+
+__device__ __forceinline__ double sum_over_wave(double v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+template <int GRAD>
+__global__ __launch_bounds__(256) void norm_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, uint32_t n_spans,
+                                                  NormScratch *scratch, ckpt_norm_result *out, double max_norm, double grad_scale) {
+    __shared__ double part[4];
+    __shared__ bool last;
+    double sum = 0;
+    for (uint32_t s = blockIdx.x; s < n_spans; s += gridDim.x) {
+        const Span span = spans[s];
+        const uint8_t *g = tensors[span.tensor].grad + span.first * sizeof(typename Element<GRAD>::one);
+        for (uint32_t i = 4 * threadIdx.x; i < span.count; i += 1024) {
+            const f32x4 v = load_upto4<GRAD>(g + i * sizeof(typename Element<GRAD>::one), span.count - i);
+#pragma unroll
+            for (int j = 0; j < 4; j++) sum += double(v[j]) * double(v[j]);
+        }
+    }
+    sum = sum_over_wave(sum);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(&scratch->partial[blockIdx.x], (part[0] + part[1]) + (part[2] + part[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    sum = 0;
+    for (uint32_t b = threadIdx.x; b < gridDim.x; b += 256) sum += __hip_atomic_load(&scratch->partial[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sum = sum_over_wave(sum);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x) return;
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    scratch->arrived = 0;
+    const bool finite = sum < __longlong_as_double(0x7FF0000000000000ll);
+    const double norm = grad_scale * sqrt(sum);
+    out->sum_squares = sum;
+    out->norm = float(norm);
+    out->scale = !finite ? 0.0f : max_norm > 0 && norm > max_norm ? float(grad_scale * (max_norm / norm)) : float(grad_scale);
+    out->nonfinite = finite ? 0 : 1;
+    out->reserved = 0;
+}
+
+// ------------------------------------------------------------------ AdamW step
+
+struct StepArgs {
+    float beta1, one_less_beta1, beta2, one_less_beta2, eps, lr, inv_bc1, inv_bc2;
+    double lr64;
+    uint64_t key;
+    const ckpt_norm_result *norm;
+};
+
+// Four elements: the moments in f32, each operation rounded by itself, so that the 8-bit moments do not depend on what a compiler fuses.
+__device__ __forceinline__ void update_moments(f32x4 g, f32x4 &m, f32x4 &v, const StepArgs &a) {
+#pragma clang fp contract(off)
+    m = m * a.beta1 + g * a.one_less_beta1;
+    v = v * a.beta2 + (g * g) * a.one_less_beta2;
+}
+// The root and the quotient by the approximate instructions (1 ulp each): the error is 1e-7 of the update, which is some 1e-4 of the weight.
+__device__ __forceinline__ f32x4 updated(f32x4 w, f32x4 m, f32x4 v, float keep, const StepArgs &a) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const float root = __builtin_amdgcn_sqrtf(v[j] * a.inv_bc2) + a.eps;
+        w[j] = w[j] * keep - a.lr * (m[j] * a.inv_bc1 * __builtin_amdgcn_rcpf(root));
+    }
+    return w;
+}
+
+// PARAM 0: no working copy. BITS: of the moments.
+template <int GRAD, int PARAM, int BITS, bool STOCHASTIC>
+__global__ __launch_bounds__(256) void adamw_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, StepArgs a) {
+    const Span span = spans[blockIdx.x];
+    const TensorEntry t = tensors[span.tensor];
+    float scale = 1.0f;
+    if (a.norm) {
+        if (a.norm->nonfinite) return;
+        scale = a.norm->scale;
+    }
+    const float keep = float(1.0 - a.lr64 * t.weight_decay);
+    // whole blocks of 32, so that the eight lanes of one are all here
+    for (uint32_t i = 4 * threadIdx.x; i < (span.count + 31) / 32 * 32; i += 1024) {
+        const uint64_t e = span.first + i;
+        const uint32_t count = i < span.count ? span.count - i : 0;
+        const f32x4 g = load_upto4<GRAD>(t.grad + e * sizeof(typename Element<GRAD>::one), count) * scale;
+        const f32x4 w = load_upto4<CKPT_F32>(t.master + e, count);
+        f32x4 m, v;
+        if constexpr (BITS == 32) {
+            m = load_upto4<CKPT_F32>(t.m + 4 * e, count);
+            v = load_upto4<CKPT_F32>(t.v + 4 * e, count);
+        } else {
+            const uint64_t block = e / 32;
+            m = fp8_values(load_bytes(t.m + e, count)) * scale_value(t.m_scale[block]);
+            v = fp8_values(load_bytes(t.v + e, count)) * scale_value(t.v_scale[block]);
+        }
+        update_moments(g, m, v, a);
+        if constexpr (BITS == 32) {
+            store_upto4<CKPT_F32>(t.m + 4 * e, m, count);
+            store_upto4<CKPT_F32>(t.v + 4 * e, v, count);
+        } else {
+            const uint64_t block = e / 32;
+            const uint32_t mb = scale_byte<CKPT_MXFP8>(most_of_8(magnitude_bits(m))), vb = scale_byte<CKPT_MXFP8>(most_of_8(magnitude_bits(v)));
+            const f32x4 ym = m * inverse_scale(mb), yv = v * inverse_scale(vb);
+            uint32_t mc, vc;
+            if constexpr (STOCHASTIC) {
+                const uint64_t r = mix64(a.key + 8 * t.first_block + e / 4);
+                const uint64_t backwards = (r << 48) | ((r << 16) & 0xFFFF00000000ull) | ((r >> 16) & 0xFFFF0000ull) | (r >> 48);
+                mc = fp8_stochastic<false>(ym, r);
+                vc = fp8_stochastic<true>(yv, backwards);
+            } else {
+                mc = fp8_nearest<false>(ym);
+                vc = fp8_nearest<true>(yv);
+            }
+            store_bytes(t.m + e, mc, count);
+            store_bytes(t.v + e, vc, count);
+            if (i % 32 == 0) { t.m_scale[block] = uint8_t(mb); t.v_scale[block] = uint8_t(vb); }
+        }
+        const f32x4 next = updated(w, m, v, keep, a);
+        store_upto4<CKPT_F32>(t.master + e, next, count);
+        if constexpr (PARAM != 0) store_upto4<PARAM>(t.param + 2 * e, next, count);
+    }
+}
+
+constexpr uint32_t kGradsALaunch = 448;
+struct GradList { const uint8_t *grad[kGradsALaunch]; };
+__global__ __launch_bounds__(kGradsALaunch) void set_grads_kernel(TensorEntry *tensors, uint32_t count, GradList list) {
+    if (threadIdx.x < count) tensors[threadIdx.x].grad = list.grad[threadIdx.x];
+}
+
+template <int GRAD, int PARAM>
+void launch_adamw(const ckpt_optim *o, const StepArgs &a, bool stochastic, hipStream_t stream) {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(o->n_spans), dim3(256), 0, stream, o->dev_tensors, o->dev_spans, a); };
+    if (o->cfg.state_bits == 32) go(adamw_kernel<GRAD, PARAM, 32, false>);
+    else if (stochastic) go(adamw_kernel<GRAD, PARAM, 8, true>);
+    else go(adamw_kernel<GRAD, PARAM, 8, false>);
+}
+template <int GRAD>
+void launch_adamw(const ckpt_optim *o, const StepArgs &a, bool stochastic, hipStream_t stream) {
+    switch (o->cfg.param_dtype) {
+        case CKPT_BF16: return launch_adamw<GRAD, CKPT_BF16>(o, a, stochastic, stream);
+        case CKPT_F16: return launch_adamw<GRAD, CKPT_F16>(o, a, stochastic, stream);
+        default: return launch_adamw<GRAD, 0>(o, a, stochastic, stream);
+    }
+}
+
+int wrong_device(const ckpt_optim *o) {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) { (void)hipGetLastError(); return refuse(CKPT_EHIP, "no current device"); }
+    return dev == o->device ? CKPT_OK : refuse(CKPT_EINVAL, "the optimizer belongs to another device than the current one");
+}
+
+int create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_optim_config *cfg, ckpt_optim **out) {
+    if (!out) return refuse(CKPT_EINVAL, "null argument");
+    *out = nullptr;
+    if (!tensors || !cfg || n == 0 || n > 0xFFFFFFFFu) return refuse(CKPT_EINVAL, "null argument or empty tensor list");
+    const uint32_t grad_bytes = element_bytes(cfg->grad_dtype);
+    if (!grad_bytes) return refuse(CKPT_EINVAL, "grad_dtype must be CKPT_F32, CKPT_BF16 or CKPT_F16");
+    if (cfg->param_dtype != 0 && cfg->param_dtype != CKPT_BF16 && cfg->param_dtype != CKPT_F16) return refuse(CKPT_EINVAL, "param_dtype must be CKPT_BF16, CKPT_F16 or 0");
+    if (cfg->state_bits != 32 && cfg->state_bits != 8) return refuse(CKPT_EINVAL, "state_bits must be 32 or 8");
+    if (cfg->reserved) return refuse(CKPT_EINVAL, "reserved field not zero");
+    std::unique_ptr<ckpt_optim> o(new ckpt_optim);
+    o->cfg = *cfg;
+    o->n = n;
+    std::vector<TensorEntry> entries(n);
+    std::vector<Span> spans;
+    DeviceRanges ranges;
+    uint64_t blocks = 0, n_spans = 0;
+    bool any = false;
+    for (size_t k = 0; k < n; k++) {
+        const ckpt_optim_tensor &t = tensors[k];
+        auto bad = [&](const char *part, const char *why) { return refuse(CKPT_EINVAL, "tensor " + std::to_string(k) + ": " + part + ": " + why); };
+        if (t.numel > 1ull << 48) return bad("numel", "too large");
+        const bool state = t.dev_master != nullptr;
+        if (t.numel) {
+            if (any && state != o->has_state) return bad("dev_master", "given for some tensors only");
+            any = true;
+            o->has_state = state;
+            struct { const char *name; const void *p; uint64_t bytes, align; } parts[] = {
+                {"dev_grad", t.dev_grad, t.numel * grad_bytes, grad_bytes},
+                {"dev_master", t.dev_master, state ? 4 * t.numel : 0, 4},
+                {"dev_param", t.dev_param, state && cfg->param_dtype ? 2 * t.numel : 0, 2},
+                {"dev_m", t.dev_m, !state ? 0 : cfg->state_bits == 32 ? 4 * t.numel : t.numel, cfg->state_bits == 32 ? 4u : 1u},
+                {"dev_v", t.dev_v, !state ? 0 : cfg->state_bits == 32 ? 4 * t.numel : t.numel, cfg->state_bits == 32 ? 4u : 1u},
+                {"dev_m_scale", t.dev_m_scale, state && cfg->state_bits == 8 ? (t.numel + 31) / 32 : 0, 1},
+                {"dev_v_scale", t.dev_v_scale, state && cfg->state_bits == 8 ? (t.numel + 31) / 32 : 0, 1},
+            };
+            for (const auto &part : parts) {
+                if (!part.bytes) continue;
+                if (const char *why = ranges.wrong(part.p, part.bytes)) return bad(part.name, why);
+                if (uint64_t(part.p) % part.align) return bad(part.name, "not aligned to its element");
+            }
+        }
+        if (!(fabs(t.weight_decay) <= 1e30)) return bad("weight_decay", "not a finite number");
+        entries[k] = TensorEntry{static_cast<const uint8_t *>(t.dev_grad), static_cast<uint8_t *>(t.dev_param), t.dev_master, static_cast<uint8_t *>(t.dev_m),
+                                 static_cast<uint8_t *>(t.dev_v), static_cast<uint8_t *>(t.dev_m_scale), static_cast<uint8_t *>(t.dev_v_scale), t.numel, blocks, t.weight_decay};
+        o->numels.push_back(t.numel);
+        blocks += (t.numel + 31) / 32;
+        n_spans += (t.numel + kSpan - 1) / kSpan;
+        if (n_spans > 1u << 24) return refuse(CKPT_EINVAL, "more than 2^36 elements");
+        for (uint64_t first = 0; first < t.numel; first += kSpan) spans.push_back(Span{uint32_t(k), uint32_t(t.numel - first < kSpan ? t.numel - first : kSpan), first});
+    }
+    o->n_spans = uint32_t(spans.size());
+    auto failed = [&](hipError_t e) {
+        (void)hipFree(o->dev_tensors); (void)hipFree(o->dev_spans); (void)hipFree(o->dev_scratch);
+        (void)hipGetLastError();
+        return refuse(e == hipErrorOutOfMemory ? CKPT_ENOMEM : CKPT_EHIP, std::string("optimizer set-up: ") + hipGetErrorString(e));
+    };
+    hipError_t e = hipGetDevice(&o->device);
+    if (e == hipSuccess) e = hipMalloc(&o->dev_tensors, n * sizeof(TensorEntry));
+    if (e == hipSuccess) e = hipMalloc(&o->dev_spans, (spans.size() + 1) * sizeof(Span));
+    if (e == hipSuccess) e = hipMalloc(&o->dev_scratch, sizeof(NormScratch));
+    if (e == hipSuccess) e = hipMemcpy(o->dev_tensors, entries.data(), n * sizeof(TensorEntry), hipMemcpyHostToDevice);
+    if (e == hipSuccess && !spans.empty()) e = hipMemcpy(o->dev_spans, spans.data(), spans.size() * sizeof(Span), hipMemcpyHostToDevice);
+    const NormScratch zero{};
+    if (e == hipSuccess) e = hipMemcpy(o->dev_scratch, &zero, sizeof zero, hipMemcpyHostToDevice);
+    if (e != hipSuccess) return failed(e);
+    *out = o.release();
+    return CKPT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ckpt_optim_create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_optim_config *cfg, ckpt_optim **out) {
+    return at_c_entry([&] { return create(tensors, n, cfg, out); });
+}
+
+int ckpt_optim_destroy(ckpt_optim *o) {
+    return at_c_entry([&] {
+        if (!o) return refuse(CKPT_EINVAL, "null argument");
+        const hipError_t e = hipDeviceSynchronize();
+        (void)hipFree(o->dev_tensors);
+        (void)hipFree(o->dev_spans);
+        (void)hipFree(o->dev_scratch);
+        delete o;
+        return e == hipSuccess ? CKPT_OK : refuse(CKPT_EHIP, hipGetErrorString(e));
+    });
+}
+
+int ckpt_optim_set_grads(ckpt_optim *o, const void *const *dev_grads, size_t n, void *stream) {
+    return at_c_entry([&] {
+        if (!o || !dev_grads) return refuse(CKPT_EINVAL, "null argument");
+        if (n != o->n) return refuse(CKPT_EINVAL, "the optimizer has " + std::to_string(o->n) + " tensors");
+        if (int r = wrong_device(o)) return r;
+        const uint32_t bytes = element_bytes(o->cfg.grad_dtype);
+        DeviceRanges ranges;
+        for (size_t k = 0; k < n; k++) {
+            if (!o->numels[k]) continue;
+            if (const char *why = ranges.wrong(dev_grads[k], o->numels[k] * bytes)) return refuse(CKPT_EINVAL, "tensor " + std::to_string(k) + ": " + why);
+            if (uint64_t(dev_grads[k]) % bytes) return refuse(CKPT_EINVAL, "tensor " + std::to_string(k) + ": not aligned to its element");
+        }
+        GradList list;
+        for (size_t first = 0; first < n; first += kGradsALaunch) {
+            const uint32_t count = uint32_t(n - first < kGradsALaunch ? n - first : kGradsALaunch);
+            for (uint32_t k = 0; k < count; k++) list.grad[k] = static_cast<const uint8_t *>(dev_grads[first + k]);
+            hipLaunchKernelGGL(set_grads_kernel, dim3(1), dim3(kGradsALaunch), 0, static_cast<hipStream_t>(stream), o->dev_tensors + first, count, list);
+        }
+        return launched();
+    });
+}
+
+int ckpt_optim_grad_norm(ckpt_optim *o, double max_norm, double grad_scale, ckpt_norm_result *dev_out, void *hip_stream) {
+    return at_c_entry([&] {
+        if (!o) return refuse(CKPT_EINVAL, "null argument");
+        if (!(max_norm == max_norm) || !(fabs(grad_scale) <= 1e30)) return refuse(CKPT_EINVAL, "max_norm or grad_scale is not a number");
+        if (int r = wrong_device(o)) return r;
+        DeviceRanges ranges;
+        if (const char *why = ranges.wrong(dev_out, sizeof *dev_out)) return refuse(CKPT_EINVAL, std::string("dev_out: ") + why);
+        if (uint64_t(dev_out) % 8) return refuse(CKPT_EINVAL, "dev_out must be 8-byte aligned");
+        const unsigned blocks = o->n_spans < 1 ? 1 : o->n_spans > kNormBlocks ? kNormBlocks : o->n_spans;
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream), o->dev_tensors, o->dev_spans, o->n_spans, o->dev_scratch, dev_out, max_norm, grad_scale);
+        };
+        switch (o->cfg.grad_dtype) {
+            case CKPT_F32: go(norm_kernel<CKPT_F32>); break;
+            case CKPT_BF16: go(norm_kernel<CKPT_BF16>); break;
+            default: go(norm_kernel<CKPT_F16>);
+        }
+        return launched();
+    });
+}
+
+int ckpt_optim_adamw_step(ckpt_optim *o, const ckpt_adamw_args *p, void *hip_stream) {
+    return at_c_entry([&] {
+        if (!o || !p) return refuse(CKPT_EINVAL, "null argument");
+        if (!o->has_state && o->n_spans) return refuse(CKPT_ESTATE, "the optimizer was created with gradients only");
+        if (!(p->beta1 >= 0 && p->beta1 < 1 && p->beta2 >= 0 && p->beta2 < 1)) return refuse(CKPT_EINVAL, "beta1 and beta2 lie in [0, 1)");
+        if (!(p->eps >= 1e-30 && p->eps <= 1e30) || !(fabs(p->lr) <= 1e30)) return refuse(CKPT_EINVAL, "eps must be at least 1e-30, lr a finite number");
+        if (p->step == 0) return refuse(CKPT_EINVAL, "steps are counted from 1");
+        if (p->rounding != CKPT_ROUND_NEAREST && p->rounding != CKPT_ROUND_STOCHASTIC) return refuse(CKPT_EINVAL, "rounding must be CKPT_ROUND_NEAREST or CKPT_ROUND_STOCHASTIC");
+        if (p->reserved) return refuse(CKPT_EINVAL, "reserved field not zero");
+        if (int r = wrong_device(o)) return r;
+        DeviceRanges ranges;
+        if (p->dev_norm) {
+            if (const char *why = ranges.wrong(p->dev_norm, sizeof *p->dev_norm)) return refuse(CKPT_EINVAL, std::string("dev_norm: ") + why);
+            if (uint64_t(p->dev_norm) % 8) return refuse(CKPT_EINVAL, "dev_norm must be 8-byte aligned");
+        }
+        if (!o->n_spans) return int(CKPT_OK);
+        StepArgs a;
+        a.beta1 = float(p->beta1);
+        a.one_less_beta1 = float(1.0 - p->beta1);
+        a.beta2 = float(p->beta2);
+        a.one_less_beta2 = float(1.0 - p->beta2);
+        a.eps = float(p->eps);
+        a.lr = float(p->lr);
+        a.lr64 = p->lr;
+        a.inv_bc1 = float(1.0 / (1.0 - pow(p->beta1, double(p->step))));
+        a.inv_bc2 = float(1.0 / (1.0 - pow(p->beta2, double(p->step))));
+        a.key = mix64(mix64(p->seed) + p->step);
+        a.norm = p->dev_norm;
+        const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        const bool stochastic = p->rounding == CKPT_ROUND_STOCHASTIC;
+        switch (o->cfg.grad_dtype) {
+            case CKPT_F32: launch_adamw<CKPT_F32>(o, a, stochastic, stream); break;
+            case CKPT_BF16: launch_adamw<CKPT_BF16>(o, a, stochastic, stream); break;
+            default: launch_adamw<CKPT_F16>(o, a, stochastic, stream);
+        }
+        return launched();
+    });
+}
+
+}  // extern "C"

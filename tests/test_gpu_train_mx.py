@@ -1,0 +1,195 @@
+"""Block-scaled quantisation and its inverse against the oracle, code by code: sizes from one element on, ragged rows, strides, unaligned starts,
+zeros, infinities and NaN, ties, both roundings; nothing outside the outputs is written."""
+import numpy as np
+import pytest
+
+from oracle import train_oracle as to
+from paper_2406_10707_amd import binding as B
+from paper_2406_10707_amd import harness
+from tests import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 256
+DTYPES = {"f32": (B.CKPT_F32, 4), "bf16": (B.CKPT_BF16, 2), "f16": (B.CKPT_F16, 2)}
+
+
+def guarded(nbytes, data=None, shift=0):
+    """(buffer, address): nbytes bytes between guards, the rest 0xEE."""
+    buf = harness.DevBuf(nbytes + 2 * GUARD)
+    host = np.full(buf.nbytes, 0xEE, np.uint8)
+    if data is not None:
+        host[GUARD + shift:GUARD + shift + nbytes] = np.frombuffer(data, np.uint8)
+    buf.upload(host)
+    return buf, buf.ptr + GUARD + shift
+
+
+def content(buf, nbytes, shift=0):
+    raw = gu.download(buf)
+    assert np.all(raw[:GUARD + shift] == 0xEE) and np.all(raw[GUARD + shift + nbytes:] == 0xEE), "written outside"
+    return raw[GUARD + shift:GUARD + shift + nbytes]
+
+
+def inputs(rows, cols, dtype, seed, special):
+    """Values of many magnitudes; `special`: whole zero blocks, ties, signed zeros, infinities, NaN, denormals. As stored, and in float64."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-6, 7, (rows, cols)).astype(np.float64)
+    x = x.astype(np.float32)
+    if special:
+        x[rng.random((rows, cols)) < 0.2] = 0
+        ties = rng.random((rows, cols)) < 0.3
+        x[ties] = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, -0.25, -5, -0.0, 1.0, 17 / 16, 19 / 16, 2.0 ** -10, 3 * 2.0 ** -10, 448.0], ties.sum())
+        for r in range(rows):
+            for b in range(0, cols, 32):
+                u = rng.random()
+                if u < 0.1:
+                    x[r, b:b + 32] = 0
+                elif u < 0.15:
+                    x[r, min(cols - 1, b + int(rng.integers(32)))] = rng.choice([np.inf, -np.inf, np.nan])
+                elif u < 0.2:
+                    x[r, b:b + 32] *= np.float32(2.0 ** -130)
+                elif u < 0.25 and dtype != "f16":
+                    x[r, b:b + 32] *= np.float32(2.0 ** 100)
+    if dtype == "f32":
+        return x, x.astype(np.float64)
+    with np.errstate(over="ignore"):
+        bits = to.half_bits(x, dtype)
+    return bits, to.half_values(bits, dtype)
+
+
+def quantized_on_device(stored, dtype, rows, cols, ld, shift, fmt, by_row, by_col, rounding, seed):
+    code, size = DTYPES[dtype]
+    src = np.zeros((rows, ld), stored.dtype)
+    src[:, :cols] = stored
+    nbytes = ((rows - 1) * ld + cols) * size
+    held, ptr = guarded(nbytes, src.tobytes()[:nbytes], shift * size)
+    outs, mats = [], []
+    for r, c, wanted in ((rows, cols, by_row), (cols, rows, by_col)):
+        if not wanted:
+            mats.append(None)
+            continue
+        cp, sp = B.mx_layout(fmt, r, c)
+        codes, cptr = guarded(r * cp)
+        scales, sptr = guarded(r * sp)
+        outs.append((codes, r * cp, scales, r * sp, r, cp, sp))
+        mats.append(B.mx_matrix(fmt, r, c, cptr, cp, sptr, sp))
+    B.mx_quantize(ptr, code, ld, mats[0], mats[1], 0, rounding=rounding, seed=seed)
+    harness.synchronize()
+    return held, mats, [(content(c, cn).reshape(r, cp), content(s, sn).reshape(r, sp)) for c, cn, s, sn, r, cp, sp in outs], outs
+
+
+SHAPES = [(1, 1), (1, 31), (1, 32), (1, 33), (2, 3), (3, 128), (5, 257), (31, 64), (32, 32), (33, 40), (64, 512), (65, 100), (130, 513), (257, 260), (7, 1030), (300, 5),
+          (1, 4099), (4099, 1)]
+
+
+@pytest.mark.parametrize("rounding", [B.CKPT_ROUND_NEAREST, B.CKPT_ROUND_STOCHASTIC])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_fp4_by_row_and_by_column(dtype, rounding):
+    for k, (rows, cols) in enumerate(SHAPES):
+        print(f"fp4 {dtype} rounding {rounding} {rows} x {cols}", flush=True)
+        stored, x = inputs(rows, cols, dtype, 100 + k, special=k % 3 != 0)
+        seed = 1000 + k
+        forms = [(True, True), (True, False), (False, True)][k % 3]
+        held, mats, got, outs = quantized_on_device(stored, dtype, rows, cols, cols + (k % 4) * 3, k % 3, to.MXFP4, *forms, rounding, seed)
+        keys = [None, None] if rounding == B.CKPT_ROUND_NEAREST else [int(to.mix(np.uint64(seed))), int(to.mix(np.uint64(~seed & to.U64)))]
+        wanted = [(y, key) for y, key, form in ((x, keys[0], forms[0]), (x.T, keys[1], forms[1])) if form]
+        for (y, key), (codes, scales), mat in zip(wanted, got, [m for m in mats if m is not None]):
+            wc, ws = to.quantize(y, to.MXFP4, key)
+            pc, ps = to.pack_rows(wc, ws, to.MXFP4, codes.shape[1], scales.shape[1])
+            assert np.array_equal(scales, ps)
+            nan = np.repeat(ws == 255, 32, axis=1)[:, : y.shape[1]]          # the codes of a NaN block do not matter
+            both = np.stack([codes & 15, codes >> 4], -1).reshape(codes.shape[0], -1)
+            want = np.stack([pc & 15, pc >> 4], -1).reshape(codes.shape[0], -1)
+            keep = np.ones(both.shape, bool)
+            keep[:, : y.shape[1]] = ~nan
+            assert np.array_equal(both[keep], want[keep])
+
+
+@pytest.mark.parametrize("rounding", [0, 1, 2, 3])
+def test_fp8_flat_and_in_rows(rounding):
+    for k, (rows, cols) in enumerate([(1, 1), (1, 5), (1, 32), (1, 97), (1, 5001), (3, 33), (40, 100), (1, 70000)]):
+        print(f"fp8 rounding {rounding} {rows} x {cols}", flush=True)
+        stored, x = inputs(rows, cols, "f32", 300 + k, special=k % 2 == 1)
+        _, _, got, _ = quantized_on_device(stored, "f32", rows, cols, cols + k % 2, k % 3, to.MXFP8, True, False, rounding, 5 + k)
+        key = int(to.mix(np.uint64(5 + k))) if rounding & 1 else None
+        wc, ws = to.quantize(x, to.MXFP8, key, bool(rounding & 2))
+        assert np.array_equal(got[0][1], ws)
+        nan = np.repeat(ws == 255, 32, axis=1)[:, :cols]
+        assert np.array_equal(got[0][0][~nan], wc[~nan])
+
+
+@pytest.mark.parametrize("fmt", [to.MXFP4, to.MXFP8])
+@pytest.mark.parametrize("dst", ["f32", "bf16", "f16"])
+def test_values_of_every_code(fmt, dst):
+    print(f"values of format {fmt} as {dst}", flush=True)
+    rng = np.random.default_rng(9)
+    for rows, cols, pad in ((1, 1, 0), (16, 256, 0), (9, 77, 5), (3, 1030, 2)):
+        codes = rng.integers(0, 16 if fmt == to.MXFP4 else 256, (rows, cols)).astype(np.uint8)
+        byte = rng.choice([0, 1, 60, 110, 127, 130, 140, 200, 253, 255], (rows, -(-cols // 32))).astype(np.uint8)
+        cp, sp = B.mx_layout(fmt, rows, cols)
+        c, s = to.pack_rows(codes, byte, fmt, cp, sp)
+        cb, cptr = guarded(c.size, c.tobytes())
+        sb, sptr = guarded(s.size, s.tobytes())
+        code, size = DTYPES[dst]
+        ld = cols + pad
+        out, optr = guarded((rows * ld - pad) * size, b"\xEE" * ((rows * ld - pad) * size), size)
+        B.mx_dequantize(B.mx_matrix(fmt, rows, cols, cptr, cp, sptr, sp), optr, code, ld, 0)
+        harness.synchronize()
+        raw = np.concatenate([content(out, (rows * ld - pad) * size, size), np.full(pad * size, 0xEE, np.uint8)]).reshape(rows, ld * size)
+        assert np.all(raw[:, cols * size:] == 0xEE)
+        got = np.ascontiguousarray(raw[:, : cols * size])
+        with np.errstate(over="ignore"):
+            want = to.values(codes, byte, fmt).astype(np.float32)
+            want = want if dst == "f32" else to.half_values(to.half_bits(want, dst), dst)
+        got = got.view(np.float32) if dst == "f32" else to.half_values(got.view(np.uint16), dst)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~np.isnan(want)], want[~np.isnan(want)])
+
+
+def test_empty_matrices_are_no_work():
+    print("empty matrices", flush=True)
+    buf = harness.DevBuf(4096)
+    for rows, cols in ((0, 5), (5, 0), (0, 0)):
+        m = B.mx_matrix(B.CKPT_MXFP4, rows, cols, None, 0, None, 0)
+        B.mx_quantize(buf.ptr, B.CKPT_F32, cols, m, None, 0)
+        B.mx_dequantize(m, buf.ptr, B.CKPT_F32, cols, 0)
+    harness.synchronize()
+
+
+def test_what_is_refused():
+    print("refusals", flush=True)
+    buf, small = harness.DevBuf(1 << 20), harness.DevBuf(1024)
+    good = dict(fmt=B.CKPT_MXFP4, rows=64, cols=256, codes=buf.ptr, code_pitch=128, scales=buf.ptr + 65536, scale_pitch=16)
+    src = buf.ptr + (512 << 10)
+
+    def refused(text, src=src, dtype=B.CKPT_F32, ld=256, rounding=0, col=None, **change):
+        with pytest.raises(B.CkptError) as e:
+            B.mx_quantize(src, dtype, ld, B.mx_matrix(**{**good, **change}), col, 0, rounding=rounding)
+        assert e.value.code == B.CKPT_EINVAL and text in e.value.text, e.value.text
+
+    refused("format", fmt=3)
+    refused("src_dtype", dtype=B.CKPT_I32)
+    refused("rounding", rounding=4)
+    refused("CKPT_ROUND_NONZERO", rounding=B.CKPT_ROUND_NONZERO)
+    refused("ld", ld=255)
+    refused("pitches", code_pitch=192)
+    refused("pitches", scale_pitch=8)
+    refused("pitches", codes=buf.ptr + 8)
+    refused("smaller than a row", code_pitch=0)
+    refused("smaller than a row", cols=257)
+    refused("out of range", rows=-1)
+    refused("null device pointer", codes=None)
+    refused("src: null", src=None)
+    refused("src is not aligned", src=src + 2)
+    refused("not device memory", src=np.zeros(1 << 20, np.uint8).ctypes.data & ~3)
+    refused("runs past its allocation", src=small.ptr)
+    refused("runs past its allocation", rows=1 << 15)
+    refused("transpose", col=B.mx_matrix(B.CKPT_MXFP4, 256, 65, buf.ptr, 128, buf.ptr + 65536, 16))
+    with pytest.raises(B.CkptError):
+        B.mx_quantize(src, B.CKPT_F32, 256, None, None, 0)
+    with pytest.raises(B.CkptError):
+        B.mx_quantize(src, B.CKPT_F32, 256, None, B.mx_matrix(B.CKPT_MXFP8, 64, 256, buf.ptr, 256, buf.ptr + 65536, 8), 0)
+    with pytest.raises(B.CkptError):
+        B.mx_dequantize(B.mx_matrix(**good), src, B.CKPT_U8, 256, 0)
+    with pytest.raises(B.CkptError):
+        B.mx_layout(9, 1, 1)
+    harness.synchronize()
