@@ -3,6 +3,8 @@
 // v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 x 128 by 128 x 16 E2M1 values: lane l holds the 32 consecutive values (16 bytes) of row
 // l mod 16 that make up block l / 16 of the step, and that block's scale byte. A and B are both kept by rows along K, so both sides
 // are read the same way; the instruction applies the two scales of a block to its partial sum.
+#include "gemm_tile.hpp"
+#include "mx_gemm_forms.hpp"
 #include "train_util.hpp"
 
 using namespace dsllm;
@@ -22,18 +24,334 @@ struct GemmArgs {
     void *c;
     int64_t ldc;
     int64_t m, n;
-    uint32_t steps;        // of 128 values
-    int accumulate;
+    uint32_t steps;        // of 256 values
+    uint32_t steps_a_split;
+    int64_t c_split;       // elements of C from one part of K to the next
+    int accumulate, vector;
 };
 
+// BYTE: which byte of the scale operands counts
+template <int BYTE>
 __device__ __forceinline__ f32x4 mfma_fp4(u32x4 a, u32x4 b, f32x4 c, uint32_t a_scale, uint32_t b_scale) {
     const i32x8 a8{int(a.x), int(a.y), int(a.z), int(a.w), 0, 0, 0, 0}, b8{int(b.x), int(b.y), int(b.z), int(b.w), 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, 0, int(a_scale), 0, int(b_scale));
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, BYTE, int(a_scale), BYTE, int(b_scale));
 }
 
-// Four waves compute 64 x 64, a wave 32 x 32, straight from memory. Rows past the end are the last row again, and not stored.
+// ------------------------------------------------------------------ tiles through LDS
+
+// The panels of a step of K (256 values, 128 bytes of codes a row) and the scales of four steps (32 bytes a row: pieces of 8 bytes, a step's, would take as
+// many requests as the panels) go from memory to LDS without passing through registers. Rows past the end of a matrix are its last row again.
+//
+// LDS layout of a panel: eight 16-byte pieces (blocks of 32 values) a row; row r keeps piece p at place p ^ f(r), so that the rows that a fragment read
+// touches lie in different banks. The loads write LDS in lane order, so the permutation is made on the global side. A fragments hold 16
+// consecutive rows, f(r) = bits 1..3 of r, rotated; B fragments come in pairs that hold 32 rows as 8 (lane / 4) + lane % 4 and that + 4, f(r) = bits 1, 3, 4,
+// rotated: with B as the first operand a lane ends up with eight consecutive columns of one row of C.
+// Half h of a step takes piece 2 q + h in the lanes 16 q to 16 q + 15 (any order of K will do that both sides share): a lane's two scales of a step are
+// then neighbours, in the upper or the lower half of an aligned word.
+// LDS layout of the scales: of eight rows the first two steps' 16 bytes one behind the other, then the other two steps' (every other eight rows the other way round).
+__device__ __forceinline__ uint32_t rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
+
+template <int BM, int BN, int NW, int STAGES>
+struct StepLoader {
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, PANELS = LA + LB;
+    static constexpr int PANEL = (BM + BN) * 128, SCALES = (BM + BN) * 32, GROUPS = (BM + BN) / 32, BYTES = STAGES * PANEL + 2 * SCALES;
+    static_assert(LA * 8 * NW == BM && LB * 8 * NW == BN && NW == 4 && BM % 32 == 0 && BN % 32 == 0, "panels divide among the waves");
+    static constexpr int PARTS = (GROUPS + NW - 1) / NW;      // loads of a wave that a window of scales takes; at most one a step
+    static_assert(STAGES == 2 ? PARTS <= 4 : STAGES == 4 && PARTS <= 2, "a step has one of them, and all are out before the panels that come with them");
+    // which part goes out ahead of the panels in a window's step `turn`, of the next window or, in the last step, the next but one
+    static constexpr int part_of(int turn) { return turn == 3 ? 0 : turn + 1; }
+    static constexpr int scales_of(int turn) { return part_of(turn) < PARTS ? 1 : 0; }
+    static constexpr int loads_of(int turn) { return scales_of(turn & 3) + PANELS; }
+    __amdgpu_buffer_rsrc_t ra, rb, rs[PARTS];
+    uint32_t off[LA + LB], scale_off[PARTS], scale_place[PARTS], wave;
+
+    __device__ __forceinline__ StepLoader(const GemmArgs &p, int64_t row, int64_t col, int lane, int wave_) : wave(wave_) {
+        const uint32_t last_a = uint32_t(min(p.m - row, int64_t(BM)) - 1), last_b = uint32_t(min(p.n - col, int64_t(BN)) - 1);
+        ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.a + row * p.a_pitch), 0, (last_a + 1) * uint32_t(p.a_pitch), 0x00020000);
+        rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.b + col * p.b_pitch), 0, (last_b + 1) * uint32_t(p.b_pitch), 0x00020000);
+        const uint32_t row0 = (lane >> 3) + 8 * wave, piece = lane & 7;
+#pragma unroll
+        for (int i = 0; i < LA + LB; i++) {
+            const uint32_t r = row0 + 8 * NW * (i < LA ? i : i - LA);
+            const uint32_t f = rotated(i < LA ? (r >> 1) & 7 : ((r >> 1) & 1) | (((r >> 3) & 3) << 1));
+            off[i] = (i < LA ? min(r, last_a) * uint32_t(p.a_pitch) : min(r, last_b) * uint32_t(p.b_pitch)) + 16 * (piece ^ f);
+        }
+#pragma unroll
+        for (int i = 0; i < PARTS; i++) {
+            const uint32_t group = (i * NW + wave) % GROUPS, r = 32 * group + 8 * (lane >> 4) + (lane & 7);      // rows of A, then of B
+            const bool of_a = 32 * group < BM;
+            scale_place[i] = STAGES * PANEL + 1024 * group;
+            scale_off[i] = (of_a ? min(r, last_a) * uint32_t(p.a_scale_pitch) : min(r - BM, last_b) * uint32_t(p.b_scale_pitch)) + 16 * (((lane >> 3) ^ (lane >> 4)) & 1);
+            const uint8_t *base = of_a ? p.a_scale + row * p.a_scale_pitch : p.b_scale + col * p.b_scale_pitch;
+            rs[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), 0, of_a ? (last_a + 1) * uint32_t(p.a_scale_pitch) : (last_b + 1) * uint32_t(p.b_scale_pitch), 0x00020000);
+        }
+    }
+    // where a row's 16 bytes of the window's first two steps lie; those of the other two: that ^ 128
+    static __device__ __forceinline__ int scale_at(int r) { return STAGES * PANEL + (r >> 3) * 256 + ((r >> 3) & 1) * 128 + (r & 7) * 16; }
+    // part of a window of scales (four steps), which goes to the place of even or odd ones; what the row has behind its end is not used
+    __device__ __forceinline__ void issue_scales(uint8_t *lds, uint32_t window, uint32_t odd, int part) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[part], (DSLLM_LDS void *)(lds + scale_place[part] + (odd & 1) * SCALES), 16, scale_off[part], 32 * window, 0, 0);
+    }
+    // instruction j of a step's panels into stage `stage`
+    __device__ __forceinline__ void issue_panels(uint8_t *lds, int stage, uint32_t step, int j) const {
+        uint8_t *place = lds + stage * PANEL + (j < LA ? j : j - LA) * 1024 * NW + 1024 * wave + (j < LA ? 0 : BM * 128);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(j < LA ? ra : rb, (DSLLM_LDS void *)place, 16, off[j], 128 * step, 0, 0);
+    }
+};
+
 template <int OUT>
-__global__ __launch_bounds__(256) void gemm_simple_kernel(GemmArgs p) {
+__device__ __forceinline__ void store_eight(const GemmArgs &p, typename Element<OUT>::one *c, int64_t columns, f32x4 lo, f32x4 hi) {
+    typedef typename Element<OUT>::one Out;
+    if (columns <= 0) return;
+    if (p.vector && columns >= 8) {
+        if constexpr (OUT == CKPT_F32) {
+            f32x4 DSLLM_GLOBAL *at = (f32x4 DSLLM_GLOBAL *)c;
+            if (p.accumulate) { lo += at[0]; hi += at[1]; }
+            at[0] = lo;
+            at[1] = hi;
+        } else {
+            typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+            bf16x8 DSLLM_GLOBAL *at = (bf16x8 DSLLM_GLOBAL *)c;
+            if (p.accumulate) {
+                const bf16x8 old = *at;
+                lo += __builtin_convertvector(__builtin_shufflevector(old, old, 0, 1, 2, 3), f32x4);
+                hi += __builtin_convertvector(__builtin_shufflevector(old, old, 4, 5, 6, 7), f32x4);
+            }
+            *at = __builtin_shufflevector(__builtin_convertvector(lo, bf16x4), __builtin_convertvector(hi, bf16x4), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        if (e >= columns) return;
+        Out DSLLM_GLOBAL *at = (Out DSLLM_GLOBAL *)c + e;
+        *at = Out((e < 4 ? lo[e & 3] : hi[e & 3]) + (p.accumulate ? float(*at) : 0.0f));
+    }
+}
+
+// Eight consecutive columns of a row of a tile of C.
+template <int OUT, bool ADD>
+__device__ __forceinline__ void store_eight_at(__amdgpu_buffer_rsrc_t c, uint32_t at, uint32_t uniform, f32x4 lo, f32x4 hi) {
+    if constexpr (OUT == CKPT_F32) {
+        if constexpr (ADD) {
+            lo += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(c, at, uniform, 0));
+            hi += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(c, at + 16, uniform, 0));
+        }
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), c, at, uniform, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), c, at + 16, uniform, 0);
+    } else {
+        typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+        if constexpr (ADD) {
+            const bf16x8 old = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(c, at, uniform, 0));
+            lo += __builtin_convertvector(__builtin_shufflevector(old, old, 0, 1, 2, 3), f32x4);
+            hi += __builtin_convertvector(__builtin_shufflevector(old, old, 4, 5, 6, 7), f32x4);
+        }
+        const bf16x8 both = __builtin_shufflevector(__builtin_convertvector(lo, bf16x4), __builtin_convertvector(hi, bf16x4), 0, 1, 2, 3, 4, 5, 6, 7);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, both), c, at, uniform, 0);
+    }
+}
+
+// Four waves, WM x WN, each computing (16 TM) x (16 TN) of the block's tile; ONE wave per SIMD or two. Nothing hides a wait but the wave's own order, so the
+// order is fixed by hand: a step of 256 values is 2 TM TN matrix instructions, and between them go the reads of the fragments (those of one half under
+// the instructions of the half before, READS instructions apart, or -READS of them behind each) and the loads of a later step, one every LOAD_EVERY. Two steps are in LDS:
+// once every wave has read its second half's fragments the stage is free and the loads of step + 2 into it start; three quarters into the step those of
+// step + 1 have landed for all. (Four steps in LDS: the loads are those of step + 4.) Tiles of more than 32 accumulators a wave name them as AGPRs in the instruction's own operands.
+//
+// 8192^3 takes 237 us = 4640 TFLOP/s with 256 x 256 tiles (gemm_long_kernel 3590): a step 2670 cycles, of which the matrix instructions are 2048, at 1.73 GHz, which the power allows (2.1 GHz
+// without the panels' loads and reads); 7000 cycles in front of a tile's 32 steps and 12,000 behind them, for the stores of C at some 4 TB/s. Scales fetched 16 bytes a row and step cost 14 us
+// more, scales read from LDS at addresses of 2 bytes 150, pieces 2 q + h without the rotation (two lanes a bank) 15.
+template <int WM, int WN, int TM, int TN, int STAGES, int READS, int LOAD_EVERY, int OUT>
+__device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrder &order) {
+    constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, FRAGS = TM + TN, HALF = TM * TN;
+    constexpr bool NAMED = TM * TN > 32;
+    typedef StepLoader<BM, BN, NW, STAGES> Loader;
+    static_assert(TN % 2 == 0, "B fragments come in pairs");
+    constexpr int PACE = READS > 0 ? READS : 1, AT_ONCE = READS > 0 ? 1 : -READS;
+    constexpr int READ_SPAN = (FRAGS + AT_ONCE - 1) / AT_ONCE * PACE;
+    constexpr int FREE_AT = READ_SPAN + 8 < HALF ? READ_SPAN + 8 : READ_SPAN + 4 < HALF ? READ_SPAN + 4 : HALF;
+    constexpr int LANDED_AT = HALF + HALF / 2;
+    constexpr int FITTING = (2 * HALF - FREE_AT + LOAD_EVERY - 1) / LOAD_EVERY;
+    constexpr int GONE = (LANDED_AT - FREE_AT + LOAD_EVERY - 1) / LOAD_EVERY;
+    static_assert(READ_SPAN <= HALF && FREE_AT <= HALF + 2, "the reads of a half lie inside the half before");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[Loader::BYTES];
+    const GemmTile t = gemm_tile(order);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN, q = lane >> 4;
+    const int64_t row = int64_t(t.tm) * BM, col = int64_t(t.tn) * BN;
+    const Loader load(p, row, col, lane, wave);
+    const int ar = lane & 15, br = 8 * (ar >> 2) + (ar & 3);
+    int at_a[2], at_b[2];
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        at_a[h] = (16 * TM * wm + ar) * 128 + 16 * ((2 * q + h) ^ rotated((ar >> 1) & 7));
+        at_b[h] = (BM + 16 * TN * wn + br) * 128 + 16 * ((2 * q + h) ^ rotated(((ar >> 1) & 1) | ((ar >> 2) << 1)));
+    }
+    const int at_sa = Loader::scale_at(16 * TM * wm + ar) + 4 * (q >> 1), at_sb = Loader::scale_at(BM + 16 * TN * wn + br) + 4 * (q >> 1);
+    const uint32_t down = 16 * (q & 1);
+    u32x4 frag[2][FRAGS];      // [half of the step]: B fragments first, then A
+    uint32_t scale[2][FRAGS];  // [step's parity]: the two halves' bytes lowest, once shifted down
+    auto read = [&](int half, int stage, int i) {
+        const uint8_t *at = lds + stage * Loader::PANEL + (i < TN ? at_b[half] + (i >> 1) * 4096 + (i & 1) * 512 : at_a[half] + (i - TN) * 2048);
+        frag[half][i] = *reinterpret_cast<const u32x4 *>(at);
+    };
+    // of a step, the `turn`th of its window
+    auto read_scale = [&](int to, uint32_t window, int turn, int i) {
+        const int of_step = (turn >> 1) * 128 + (turn & 1) * 8;
+        const uint8_t *at = lds + (window & 1) * Loader::SCALES + (i < TN ? (at_sb ^ of_step) + (i >> 1) * 1024 + (i & 1) * 64 : (at_sa ^ of_step) + (i - TN) * 512);
+        scale[to][i] = *reinterpret_cast<const uint32_t *>(at);
+    };
+    // with named accumulators pinned where it stands: no matrix instruction in asm may follow at once that reads it
+    auto shift_scale = [&](int which, int i) {
+        if constexpr (NAMED) asm volatile("v_lshrrev_b32 %0, %1, %0" : "+v"(scale[which][i]) : "v"(down));
+        else scale[which][i] >>= down;
+    };
+    // fragment i of the next step's first half is read behind matrix instruction READ_AT(i) of this step, its scales are shifted SHIFT_LATER instructions after that
+    constexpr int SHIFT_LATER = NAMED ? 8 : 4;
+    auto read_at = [](int i) constexpr { return LANDED_AT + i / AT_ONCE * PACE; };
+    auto shift_at = [=](int i) constexpr { return read_at(i) + SHIFT_LATER; };
+    static_assert(!NAMED || [](auto at) constexpr {      // fragment i (A's from TN on) first counts in instruction i (TN (i - TN)) of the next step
+        for (int i = 0; i < FRAGS; i++)
+            if (at(i) >= 2 * HALF + (i < TN ? 0 : TN * (i - TN)) - 1) return false;
+        return true;
+    }(shift_at), "scales are shifted before they count");
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+    // Steps are counted from the part of K's first, which is a multiple of 4. Past the end the last step is loaded again, into a stage nothing reads.
+    const uint32_t first = blockIdx.y * p.steps_a_split, steps = min(p.steps - first, p.steps_a_split), windows = first / 4;
+    // load i of those that go out in step 4 window + turn: one of a later window of scales (not in every step), then the panels of the step STAGES later
+    auto issue = [&](uint32_t window, auto turn, int i) {
+        constexpr int part = Loader::part_of(turn), scales = Loader::scales_of(turn);
+        if (scales && i == 0) load.issue_scales(lds, windows + window + 1 + (turn + 1) / 4, window + 1 + (turn + 1) / 4, part);
+        else load.issue_panels(lds, turn % STAGES, first + min(4 * window + turn + STAGES, steps - 1), i - scales);
+    };
+#pragma unroll
+    for (int i = 0; i < Loader::PARTS; i++) load.issue_scales(lds, windows, 0, i);
+#pragma unroll
+    for (int s = 0; s < STAGES; s++) {
+        if (s == STAGES - 1) load.issue_scales(lds, windows + 1, 1, 0);
+#pragma unroll
+        for (int i = 0; i < Loader::PANELS; i++) load.issue_panels(lds, s, first + min(uint32_t(s), steps - 1), i);
+    }
+    wait_loads_and_meet<(STAGES - 1) * Loader::PANELS + 1>();
+#pragma unroll
+    for (int i = 0; i < FRAGS; i++) { read(0, 0, i); read_scale(0, 0, 0, i); }
+#pragma unroll
+    for (int i = 0; i < FRAGS; i++)
+        if (!NAMED || shift_at(i) < 2 * HALF) shift_scale(0, i);
+    if constexpr (NAMED) {
+        // set by ordinary instructions, read by the asm below, for which the compiler inserts no wait states
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[i][j]));
+        asm volatile("s_nop 7");
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    auto do_step = [&](auto turn_, uint32_t window) {
+        constexpr int turn = turn_, stage = turn % STAGES, next = (turn + 1) % STAGES, now = turn & 1, COUNT = Loader::loads_of(turn);
+        constexpr int UNDER_WAY = (GONE < COUNT ? GONE : COUNT) + (STAGES == 4 ? Loader::loads_of(turn + 3) + Loader::loads_of(turn + 2) : 0);
+        const uint32_t window_next = window + (turn + 1) / 4;
+        for_each_of([&](auto index) {
+            constexpr int at = index, half = at / HALF, i = at % HALF / TN, j = i & 1 ? TN - 1 - at % TN : at % TN;
+            if constexpr (at == FREE_AT) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if constexpr (at == LANDED_AT) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(UNDER_WAY) : "memory");
+            if constexpr (NAMED && half == 0)
+                asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                             : "+a"(acc[i][j]) : "v"(frag[half][j]), "v"(frag[half][TN + i]), "v"(scale[now][j]), "v"(scale[now][TN + i]));
+            else if constexpr (NAMED)
+                asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                             : "+a"(acc[i][j]) : "v"(frag[half][j]), "v"(frag[half][TN + i]), "v"(scale[now][j]), "v"(scale[now][TN + i]));
+            else acc[i][j] = mfma_fp4<half>(frag[half][j], frag[half][TN + i], acc[i][j], scale[now][j], scale[now][TN + i]);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; u++) {
+                if (at < HALF && at % PACE == 0 && at / PACE * AT_ONCE + u < FRAGS) read(1, stage, at / PACE * AT_ONCE + u);
+                if (at >= LANDED_AT && (at - LANDED_AT) % PACE == 0 && (at - LANDED_AT) / PACE * AT_ONCE + u < FRAGS) {
+                    read(0, next, (at - LANDED_AT) / PACE * AT_ONCE + u);
+                    read_scale(now ^ 1, window_next, (turn + 1) % 4, (at - LANDED_AT) / PACE * AT_ONCE + u);
+                }
+            }
+#pragma unroll
+            for (int f = 0; f < FRAGS; f++) {
+                if (shift_at(f) == at) shift_scale(now ^ 1, f);
+                if (NAMED && shift_at(f) == at + 2 * HALF) shift_scale(now, f);      // of the reads of the step before
+            }
+            if constexpr (at >= FREE_AT && (at - FREE_AT) % LOAD_EVERY == 0 && (at - FREE_AT) / LOAD_EVERY < COUNT)
+                issue(window, turn_, (at - FREE_AT) / LOAD_EVERY);
+            __builtin_amdgcn_sched_barrier(0);
+        }, std::make_integer_sequence<int, 2 * HALF>{});
+        // what there was no matrix instruction left for
+#pragma unroll
+        for (int i = FITTING; i < COUNT; i++) issue(window, turn_, i);
+#pragma unroll
+        for (int i = (2 * HALF - LANDED_AT + PACE - 1) / PACE * AT_ONCE; i < FRAGS; i++) { read(0, next, i); read_scale(now ^ 1, window_next, (turn + 1) % 4, i); }
+        if constexpr (!NAMED)
+#pragma unroll
+            for (int i = 0; i < FRAGS; i++)
+                if (shift_at(i) >= 2 * HALF) shift_scale(now ^ 1, i);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (uint32_t window = 0;; window++) {
+        do_step(std::integral_constant<int, 0>{}, window);
+        if (4 * window + 1 == steps) break;
+        do_step(std::integral_constant<int, 1>{}, window);
+        if (4 * window + 2 == steps) break;
+        do_step(std::integral_constant<int, 2>{}, window);
+        if (4 * window + 3 == steps) break;
+        do_step(std::integral_constant<int, 3>{}, window);
+        if (4 * window + 4 == steps) break;
+    }
+    // the last matrix instructions' results are readable, and no load to LDS outlives the block
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0)" ::: "memory");
+    typedef typename Element<OUT>::one Out;
+    const int64_t part = blockIdx.y * p.c_split;
+    if (p.vector && row + BM <= p.m && col + BN <= p.n) {
+        // A whole tile: few instructions a store. (With the bounds of each store beside it this was 40 KB of code that every block fetched anew, 190 cycles a store.)
+        Out *tile = static_cast<Out *>(p.c) + part + row * p.ldc + col;
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(tile, 0, 0xFFFFFFFFu, 0x00020000);
+        const uint32_t pitch = uint32_t(p.ldc) * sizeof(Out), lane_at = (wm * 16 * TM + ar) * pitch + (wn * 16 * TN + 8 * q) * sizeof(Out);
+        auto store_tile = [&](auto add) {
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+#pragma unroll
+                for (int j = 0; j < TN; j += 2) {
+                    // in their registers up to here: copied out all at once they would spill
+                    if constexpr (NAMED) asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
+                    store_eight_at<OUT, add>(rc, lane_at + 16 * j * sizeof(Out), 16 * i * pitch, acc[i][j], acc[i][j + 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        if (p.accumulate) store_tile(std::true_type{});
+        else store_tile(std::false_type{});
+        return;
+    }
+    const int64_t c_row = row + wm * 16 * TM + ar, c_col = col + wn * 16 * TN + 8 * q;
+    Out *c = static_cast<Out *>(p.c) + part + c_row * p.ldc + c_col;
+#pragma unroll
+    for (int i = 0; i < TM; i++) {
+        const bool inside = c_row + 16 * i < p.m;
+#pragma unroll
+        for (int j = 0; j < TN; j += 2) {
+            if constexpr (NAMED) asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
+            if (inside) store_eight<OUT>(p, c + 16 * i * p.ldc + 16 * j, p.n - c_col - 16 * j, acc[i][j], acc[i][j + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+// TOGETHER blocks share a compute unit. The bodies are the device's only: the host's pass needs no more than the names.
+template <int TOGETHER, int WM, int WN, int TM, int TN, int STAGES, int READS, int LOAD_EVERY, int OUT>
+__global__ __launch_bounds__(256, TOGETHER) void gemm_tile_kernel(GemmArgs p, TileOrder order) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    gemm_tile_body<WM, WN, TM, TN, STAGES, READS, LOAD_EVERY, OUT>(p, order);
+#endif
+}
+
+// For rows of more than 2^23 bytes, which the loads above cannot address: four waves compute 64 x 64, a wave 32 x 32, straight from memory with 64-bit addresses. Rows
+// past the end are the last row again, and not stored.
+template <int OUT>
+__global__ __launch_bounds__(256) void gemm_long_kernel(GemmArgs p) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
     const int64_t row0 = int64_t(blockIdx.y) * 64 + 32 * (wave & 1), col0 = int64_t(blockIdx.x) * 64 + 32 * (wave >> 1);
     const uint8_t *a[2], *b[2], *as[2], *bs[2];
@@ -46,7 +364,7 @@ __global__ __launch_bounds__(256) void gemm_simple_kernel(GemmArgs p) {
         bs[i] = p.b_scale + c * p.b_scale_pitch + q;
     }
     f32x4 acc[2][2] = {};
-    for (uint32_t s = 0; s < p.steps; s++) {
+    for (uint32_t s = 0; s < 2 * p.steps; s++) {
         u32x4 fa[2], fb[2];
         uint32_t sa[2], sb[2];
 #pragma unroll
@@ -59,7 +377,7 @@ __global__ __launch_bounds__(256) void gemm_simple_kernel(GemmArgs p) {
 #pragma unroll
         for (int i = 0; i < 2; i++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) acc[i][j] = mfma_fp4(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
+            for (int j = 0; j < 2; j++) acc[i][j] = mfma_fp4<0>(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
     }
     typedef typename Element<OUT>::one Out;
 #pragma unroll
@@ -73,6 +391,22 @@ __global__ __launch_bounds__(256) void gemm_simple_kernel(GemmArgs p) {
                 Out DSLLM_GLOBAL *at = (Out DSLLM_GLOBAL *)p.c + r * p.ldc + c;
                 *at = Out(acc[i][j][e] + (p.accumulate ? float(*at) : 0.0f));
             }
+}
+
+// In the order of kMxGemmForms
+template <int OUT>
+void launch_form(int form, const GemmArgs &p, hipStream_t stream) {
+    const MxGemmForm &f = kMxGemmForms[form];
+    const uint32_t tiles_m = uint32_t((p.m + f.bm - 1) / f.bm), tiles_n = uint32_t((p.n + f.bn - 1) / f.bn);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n), dim3(256), 0, stream, p, TileOrder(tiles_m, tiles_n, true)); };
+    switch (form) {
+        case 0: go(gemm_tile_kernel<1, 2, 2, 8, 8, 2, 2, 4, OUT>); break;
+        case 1: go(gemm_tile_kernel<1, 2, 2, 6, 6, 2, 1, 3, OUT>); break;
+        case 2: go(gemm_tile_kernel<2, 2, 2, 4, 4, 2, 1, 1, OUT>); break;
+        case 3: go(gemm_tile_kernel<2, 2, 2, 2, 4, 2, -2, 1, OUT>); break;
+        case 4: go(gemm_tile_kernel<2, 2, 2, 2, 2, 4, -2, 1, OUT>); break;
+        default: go(gemm_tile_kernel<3, 2, 2, 2, 2, 2, -2, 1, OUT>); break;
+    }
 }
 
 int gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t dtype, int64_t ldc, int32_t accumulate, void *workspace, uint64_t workspace_bytes,
@@ -92,12 +426,21 @@ int gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t dtyp
     if (uint64_t(c) % bytes) return refuse(CKPT_EINVAL, "C is not aligned to its element");
     if (const char *why = ranges.wrong(c, (uint64_t(m - 1) * ldc + n) * bytes)) return refuse(CKPT_EINVAL, std::string("C: ") + why);
     (void)workspace; (void)workspace_bytes;
+    const bool vector = uint64_t(c) % 16 == 0 && ldc * bytes % 16 == 0 && ldc <= 1 << 21;      // 256 rows in 32-bit offsets
+    const uint32_t steps = uint32_t((k + 255) / 256);
     GemmArgs p{static_cast<const uint8_t *>(a->codes), static_cast<const uint8_t *>(b->codes), static_cast<const uint8_t *>(a->scales), static_cast<const uint8_t *>(b->scales),
-               a->code_pitch, b->code_pitch, a->scale_pitch, b->scale_pitch, c, ldc, m, n, uint32_t((k + 127) / 128), accumulate};
+               a->code_pitch, b->code_pitch, a->scale_pitch, b->scale_pitch, c, ldc, m, n, steps, steps, 0, accumulate, vector};
+    const int form = steps && a->code_pitch <= 1u << 23 && b->code_pitch <= 1u << 23 && a->scale_pitch <= 1u << 23 && b->scale_pitch <= 1u << 23
+                         ? mx_gemm_form(uint64_t(m), uint64_t(n), uint64_t(k), dtype == CKPT_F32) : -1;
+    if (form >= 0) {
+        if (dtype == CKPT_F32) launch_form<CKPT_F32>(form, p, stream);
+        else launch_form<CKPT_BF16>(form, p, stream);
+        return launched();
+    }
     const dim3 grid(unsigned((n + 63) / 64), unsigned((m + 63) / 64));
     if (grid.y > 65535) return refuse(CKPT_EINVAL, "too many rows");
-    if (dtype == CKPT_F32) hipLaunchKernelGGL(gemm_simple_kernel<CKPT_F32>, grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL(gemm_simple_kernel<CKPT_BF16>, grid, dim3(256), 0, stream, p);
+    if (dtype == CKPT_F32) hipLaunchKernelGGL(gemm_long_kernel<CKPT_F32>, grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(gemm_long_kernel<CKPT_BF16>, grid, dim3(256), 0, stream, p);
     return launched();
 }
 

@@ -10,6 +10,7 @@
 
 #include "../../include/ckpt_proxy.h"
 #include "gemm_forms.hpp"
+#include "gemm_tile.hpp"
 
 using namespace dsllm;
 
@@ -144,54 +145,6 @@ __global__ __launch_bounds__(64) void devcopy_kernel(u32x4 *__restrict__ dst, co
 // A fragments hold 16 consecutive rows, f(r) = bits 1..3 of r. B fragments come in pairs that hold 32 rows as
 // 8 (lane / 4) + lane % 4 and that + 4, f(r) = bits 1, 3, 4: with B as the first operand a lane then ends up with eight
 // consecutive columns of one row of C, one 16-byte store (8-byte stores of 32-byte pieces cost 3 % of the whole).
-#define DSLLM_LDS __attribute__((address_space(3)))
-#define DSLLM_GLB __attribute__((address_space(1)))
-
-struct GemmTile { int tm, tn; };
-
-// Which tile a block computes. Consecutive block ids go to different XCDs (8 of them, each with its own L2): each XCD is given
-// a contiguous range of tiles, walked in strips 8 tiles tall so that neighbours share A and B panels. With a short K the
-// stores of C are what counts, and those go better in block order where 8 does not divide the number of tiles (7808 x 3968 x
-// 128 18.2 us, by XCD 18.9).
-// The host prepares the divisions: three of them, on scalars, were 90 of the 150 instructions in front of a block's first load
-// (and a branch costs some 40 cycles, so there is none). Products of 4 to 6 us take 4 % less than with divisions in the kernel, of
-// 6 to 10 us 2 %, of 10 to 20 us 1 % (300 products; 1024 x 3072 x 768 7.7 -> 7.5 us, 896 x 3072 x 64 4.1 -> 3.5); those of
-// 3 us are bound by the launches.
-struct TileOrder {
-    uint32_t xcd_bits, xcd_shift;            // of a block id: its XCD, what is left of it (0, 0: tiles go in the blocks' own order)
-    uint32_t each, more;                     // tiles of every XCD; how many XCDs have one tile more
-    uint32_t per_strip, strip_inverse;       // tiles of a full strip
-    uint32_t full_strips, last_rows, last_inverse;       // the last strip may be less than 8 tall
-
-    static uint32_t inverse(uint32_t d) { return 0xFFFFFFFFu / d; }
-    // x / d: the upper half of x times the inverse is that or one less
-    static __host__ __device__ __forceinline__ uint32_t divided(uint32_t x, uint32_t d, uint32_t inverse) {
-        const uint32_t q = uint32_t((uint64_t(x) * inverse) >> 32);
-        return x - q * d >= d ? q + 1 : q;
-    }
-    TileOrder(uint32_t tiles_m, uint32_t tiles_n, bool by_xcd) {
-        const uint32_t n = tiles_m * tiles_n;
-        const bool in_order = !by_xcd && n % 8;
-        xcd_bits = in_order ? 0 : 7;
-        xcd_shift = in_order ? 0 : 3;
-        each = n / 8;
-        more = n % 8;
-        per_strip = 8 * tiles_n;
-        strip_inverse = inverse(per_strip);
-        full_strips = tiles_m / 8;
-        last_rows = tiles_m % 8 ? tiles_m % 8 : 8;
-        last_inverse = inverse(last_rows);
-    }
-};
-
-__device__ __forceinline__ GemmTile gemm_tile(const TileOrder &o) {
-    const uint32_t xcd = blockIdx.x & o.xcd_bits, tile = xcd * o.each + min(xcd, o.more) + (blockIdx.x >> o.xcd_shift);
-    const uint32_t s = TileOrder::divided(tile, o.per_strip, o.strip_inverse), in_s = tile - s * o.per_strip;
-    const uint32_t rows_here = s < o.full_strips ? 8 : o.last_rows;
-    const uint32_t col = TileOrder::divided(in_s, rows_here, s < o.full_strips ? 1u << 29 : o.last_inverse);
-    return GemmTile{int(8 * s + in_s - col * rows_here), int(col)};
-}
-
 // One wave's eight rows of a panel per instruction; NW waves share a panel. KEPT: a lane's offset for each instruction stays in
 // a register of its own; otherwise the instruction's part is a scalar addition for every load, which is issued in the shadow
 // of a matrix instruction. Where that shadow is short the registers are faster (128 x 128 tiles: 3 %), with 256 x 256 tiles
@@ -235,13 +188,6 @@ struct PanelLoader {
         }
     }
 };
-
-// This wave's loads are in LDS but for the latest N, its LDS reads are over, and every wave of the block is here.
-template <int N>
-__device__ __forceinline__ void wait_loads_and_meet() {
-    static_assert(N >= 0 && N < 64, "vmcnt has six bits");
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
 
 __device__ __forceinline__ void store_columns(uint16_t *c, f32x4 lo, f32x4 hi) {
     const bf16x4 a = __builtin_convertvector(lo, bf16x4), b = __builtin_convertvector(hi, bf16x4);
@@ -338,9 +284,6 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void gemm_bf16_kernel(const uint
             for (int j = 0; j < TN; j += 2) store_columns(c + size_t(16 * i) * N + 16 * j, acc[i][j], acc[i][j + 1]);
     }
 }
-
-template <class F, int... I>
-__device__ __forceinline__ void for_each_of(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 
 // The other products: WM x WN waves, each computing (16 TM) x (16 TN) of the block's tile, ONE wave per SIMD or two. Nothing
 // hides a wait but the wave's own order, so the order is fixed by hand: a step of 64 K values is 2 TM TN MFMAs, and
