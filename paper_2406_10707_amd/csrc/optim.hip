@@ -1,7 +1,9 @@
 // The update phase over a list of tensors (include/ckpt_train.h): the norm of all gradients and the AdamW step, a launch each.
 #include <math.h>
 
+#include <algorithm>
 #include <memory>
+#include <type_traits>
 #include <vector>
 
 #include "train_util.hpp"
@@ -25,10 +27,10 @@ struct Span {
     uint32_t tensor, count;
     uint64_t first;
 };
-constexpr uint32_t kSpan = 4096, kNormBlocks = 2048;
+constexpr uint32_t kSpan = 4096, kNormBlocks = 1024;
 
 struct NormScratch {
-    double partial[kNormBlocks];
+    uint64_t partial[kNormBlocks];      // bits of doubles
     uint32_t arrived;
 };
 
@@ -56,38 +58,79 @@ __device__ __forceinline__ double sum_over_wave(double v) {
     return v;
 }
 
-template <int GRAD>
-__global__ __launch_bounds__(256) void norm_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, uint32_t n_spans,
+// One pass over all gradients, squares in 64 bits (no f32 gradient overflows them, and only an infinity or a NaN makes the sum one); a block's sum goes to its place in the scratch memory, the
+// block that finds itself the last adds them up in order. Bound by memory: 124 M f32 gradients 72 us = 6.9 TB/s, 405 M bf16 121 us = 6.7 TB/s. Some 8 MB have to be under way: f32 with 512 blocks of 256
+// (1024: 76 us, 256: 110), two bytes with 1024 of 512 (512: 160). Counting itself is some 10 ns a block, so short lists have a block for every sixteen spans (4.5 M bf16: 256 blocks 10 us, 1024 16).
+inline uint32_t norm_blocks(uint32_t n_spans, uint32_t most) {
+    const uint32_t wanted = n_spans / 16 < 256 ? 256 : n_spans / 16 > most ? most : n_spans / 16;
+    return n_spans < 1 ? 1 : n_spans < wanted ? n_spans : wanted;
+}
+
+template <int N>
+__device__ __forceinline__ double sum_of_parts(const double (&part)[N]) {
+    double s = part[0];
+#pragma unroll
+    for (int i = 1; i < N; i++) s += part[i];
+    return s;
+}
+
+// 4 PIECE elements in accesses of 16 bytes, at any element's address
+template <int GRAD, uint32_t PIECE>
+__device__ __forceinline__ void load_piece(f32x4 *v, const uint8_t *p) {
+    if constexpr (PIECE == 1) v[0] = load4<GRAD>(p);
+    else {
+        typedef typename Element<GRAD>::one eight __attribute__((ext_vector_type(8)));
+        typedef eight eight_bytealigned __attribute__((aligned(1)));
+        const eight e = __builtin_nontemporal_load((const eight_bytealigned DSLLM_GLOBAL *)p);
+        v[0] = __builtin_convertvector(__builtin_shufflevector(e, e, 0, 1, 2, 3), f32x4);
+        v[1] = __builtin_convertvector(__builtin_shufflevector(e, e, 4, 5, 6, 7), f32x4);
+    }
+}
+
+template <int GRAD, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, uint32_t n_spans,
                                                   NormScratch *scratch, ckpt_norm_result *out, double max_norm, double grad_scale) {
-    __shared__ double part[4];
+    __shared__ double part[THREADS / 64];
     __shared__ bool last;
+    constexpr uint32_t kPiece = GRAD == CKPT_F32 ? 1 : 2, kPasses = kSpan / (4 * THREADS), kBytes = sizeof(typename Element<GRAD>::one);
     double sum = 0;
+    auto add = [&](f32x4 v) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum += double(v[j]) * double(v[j]);
+    };
     for (uint32_t s = blockIdx.x; s < n_spans; s += gridDim.x) {
         const Span span = spans[s];
-        const uint8_t *g = tensors[span.tensor].grad + span.first * sizeof(typename Element<GRAD>::one);
-        for (uint32_t i = 4 * threadIdx.x; i < span.count; i += 1024) {
-            const f32x4 v = load_upto4<GRAD>(g + i * sizeof(typename Element<GRAD>::one), span.count - i);
+        const uint8_t *g = tensors[span.tensor].grad + span.first * kBytes;
+        if (span.count == kSpan) {
+            f32x4 v[kPasses];
 #pragma unroll
-            for (int j = 0; j < 4; j++) sum += double(v[j]) * double(v[j]);
+            for (uint32_t k = 0; k < kPasses; k += kPiece) load_piece<GRAD, kPiece>(&v[k], g + (4 * kPiece * (threadIdx.x + THREADS * (k / kPiece))) * kBytes);
+#pragma unroll
+            for (uint32_t k = 0; k < kPasses; k++) add(v[k]);
+        } else {
+            for (uint32_t i = 4 * threadIdx.x; i < span.count; i += 4 * THREADS) add(load_upto4<GRAD>(g + i * kBytes, span.count - i));
         }
     }
     sum = sum_over_wave(sum);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        __hip_atomic_store(&scratch->partial[blockIdx.x], (part[0] + part[1]) + (part[2] + part[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        // The partial sum is at the place where all compute units see it once the exchange has returned, and only then is the block counted: the order comes from waiting for the
+        // value, not from a release (which writes the whole L2 back: 36 ns a block, one behind the other).
+        const uint64_t before = __hip_atomic_exchange(&scratch->partial[blockIdx.x], uint64_t(__double_as_longlong(sum_of_parts(part))), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::"v"(before) : "memory");
+        last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     }
     __syncthreads();
     if (!last) return;
     sum = 0;
-    for (uint32_t b = threadIdx.x; b < gridDim.x; b += 256) sum += __hip_atomic_load(&scratch->partial[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (uint32_t b = threadIdx.x; b < gridDim.x; b += THREADS) sum += __longlong_as_double(int64_t(__hip_atomic_load(&scratch->partial[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
     sum = sum_over_wave(sum);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x) return;
-    sum = (part[0] + part[1]) + (part[2] + part[3]);
-    scratch->arrived = 0;
+    sum = sum_of_parts(part);
+    __hip_atomic_store(&scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool finite = sum < __longlong_as_double(0x7FF0000000000000ll);
     const double norm = grad_scale * sqrt(sum);
     out->sum_squares = sum;
@@ -122,58 +165,88 @@ __device__ __forceinline__ f32x4 updated(f32x4 w, f32x4 m, f32x4 v, float keep, 
     return w;
 }
 
+// Bound by memory: 32-bit moments move 28 or 30 bytes an element, 8-bit ones 16.1 with gradients in 16 bits. Blocks of one wave in address order keep the chip in a narrow front of each of the seven to
+// nine streams, and shared memory that nothing uses keeps the front narrower still where the grid is larger than the chip: 124 M elements with f32 gradients 609 us, with room for twelve waves to a
+// compute unit 570 = 6.5 TB/s, for seven 596 (two groups a lane: 620, 604, 592; blocks of four waves that loop over a span 665). 8-bit moments need more waves, or more a lane: 405 M
+// elements 1057 us with one group, with two 1084 and, with room for twenty waves, 1055 = 6.2 TB/s (twelve waves: 1760 and 1171); rounding to nearest 1046.
+constexpr unsigned kFreeBlocks = 256 * 36;
+constexpr uint32_t kSpansALaunch = 1u << 21;      // a grid has fewer than 2^32 work-items
+// A wave a block, GROUPS groups of four elements a lane, 256 elements apart; kSpan / (256 GROUPS) blocks a span. Every block of 32 elements lies in eight neighbouring lanes.
 // PARAM 0: no working copy. BITS: of the moments.
-template <int GRAD, int PARAM, int BITS, bool STOCHASTIC>
-__global__ __launch_bounds__(256) void adamw_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, StepArgs a) {
-    const Span span = spans[blockIdx.x];
-    const TensorEntry t = tensors[span.tensor];
+template <int GRAD, int PARAM, int BITS, bool STOCHASTIC, int GROUPS>
+__global__ __launch_bounds__(64) void adamw_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, StepArgs a) {
+    constexpr uint32_t kWave = 256 * GROUPS, kBlocks = kSpan / kWave;
+    const Span span = spans[blockIdx.x / kBlocks];
+    const uint32_t start = blockIdx.x % kBlocks * kWave;
+    if (start >= span.count) return;
+    const TensorEntry &t = tensors[span.tensor];
     float scale = 1.0f;
     if (a.norm) {
         if (a.norm->nonfinite) return;
         scale = a.norm->scale;
     }
     const float keep = float(1.0 - a.lr64 * t.weight_decay);
-    // whole blocks of 32, so that the eight lanes of one are all here
-    for (uint32_t i = 4 * threadIdx.x; i < (span.count + 31) / 32 * 32; i += 1024) {
-        const uint64_t e = span.first + i;
-        const uint32_t count = i < span.count ? span.count - i : 0;
-        const f32x4 g = load_upto4<GRAD>(t.grad + e * sizeof(typename Element<GRAD>::one), count) * scale;
-        const f32x4 w = load_upto4<CKPT_F32>(t.master + e, count);
-        f32x4 m, v;
-        if constexpr (BITS == 32) {
-            m = load_upto4<CKPT_F32>(t.m + 4 * e, count);
-            v = load_upto4<CKPT_F32>(t.v + 4 * e, count);
-        } else {
-            const uint64_t block = e / 32;
-            m = fp8_values(load_bytes(t.m + e, count)) * scale_value(t.m_scale[block]);
-            v = fp8_values(load_bytes(t.v + e, count)) * scale_value(t.v_scale[block]);
-        }
-        update_moments(g, m, v, a);
-        if constexpr (BITS == 32) {
-            store_upto4<CKPT_F32>(t.m + 4 * e, m, count);
-            store_upto4<CKPT_F32>(t.v + 4 * e, v, count);
-        } else {
-            const uint64_t block = e / 32;
-            const uint32_t mb = scale_byte<CKPT_MXFP8>(most_of_8(magnitude_bits(m))), vb = scale_byte<CKPT_MXFP8>(most_of_8(magnitude_bits(v)));
-            const f32x4 ym = m * inverse_scale(mb), yv = v * inverse_scale(vb);
-            uint32_t mc, vc;
-            if constexpr (STOCHASTIC) {
-                const uint64_t r = mix64(a.key + 8 * t.first_block + e / 4);
-                const uint64_t backwards = (r << 48) | ((r << 16) & 0xFFFF00000000ull) | ((r >> 16) & 0xFFFF0000ull) | (r >> 48);
-                mc = fp8_stochastic<false>(ym, r);
-                vc = fp8_stochastic<true>(yv, backwards);
+    const uint64_t e0 = span.first + start;
+    const uint32_t left = span.count - start;
+    auto work = [&](auto whole) {
+        f32x4 g[GROUPS], w[GROUPS], m[GROUPS], v[GROUPS];
+        uint32_t mc[GROUPS], vc[GROUPS], mb[GROUPS], vb[GROUPS], count[GROUPS];
+#pragma unroll
+        for (int k = 0; k < GROUPS; k++) {
+            const uint32_t i = 256 * k + 4 * threadIdx.x;
+            const uint64_t e = e0 + i;
+            count[k] = whole ? 4 : i < left ? left - i : 0;
+            g[k] = load_upto4<GRAD>(t.grad + e * sizeof(typename Element<GRAD>::one), count[k]);
+            w[k] = load_upto4<CKPT_F32>(t.master + e, count[k]);
+            if constexpr (BITS == 32) {
+                m[k] = load_upto4<CKPT_F32>(t.m + 4 * e, count[k]);
+                v[k] = load_upto4<CKPT_F32>(t.v + 4 * e, count[k]);
             } else {
-                mc = fp8_nearest<false>(ym);
-                vc = fp8_nearest<true>(yv);
+                mc[k] = load_bytes(t.m + e, count[k]);
+                vc[k] = load_bytes(t.v + e, count[k]);
+                mb[k] = i < left ? ((const uint8_t DSLLM_GLOBAL *)t.m_scale)[e / 32] : 0;
+                vb[k] = i < left ? ((const uint8_t DSLLM_GLOBAL *)t.v_scale)[e / 32] : 0;
             }
-            store_bytes(t.m + e, mc, count);
-            store_bytes(t.v + e, vc, count);
-            if (i % 32 == 0) { t.m_scale[block] = uint8_t(mb); t.v_scale[block] = uint8_t(vb); }
         }
-        const f32x4 next = updated(w, m, v, keep, a);
-        store_upto4<CKPT_F32>(t.master + e, next, count);
-        if constexpr (PARAM != 0) store_upto4<PARAM>(t.param + 2 * e, next, count);
-    }
+#pragma unroll
+        for (int k = 0; k < GROUPS; k++) {
+            const uint32_t i = 256 * k + 4 * threadIdx.x;
+            const uint64_t e = e0 + i;
+            if constexpr (BITS == 8) {
+                m[k] = fp8_values(mc[k]) * scale_value(mb[k]);
+                v[k] = fp8_values(vc[k]) * scale_value(vb[k]);
+            }
+            update_moments(g[k] * scale, m[k], v[k], a);
+            if constexpr (BITS == 32) {
+                store_upto4<CKPT_F32>(t.m + 4 * e, m[k], count[k]);
+                store_upto4<CKPT_F32>(t.v + 4 * e, v[k], count[k]);
+            } else {
+                const uint32_t mb = scale_byte<CKPT_MXFP8>(most_of_8(magnitude_bits(m[k]))), vb = scale_byte<CKPT_MXFP8>(most_of_8(magnitude_bits(v[k])));
+                const f32x4 ym = m[k] * inverse_scale(mb), yv = v[k] * inverse_scale(vb);
+                uint32_t mc, vc;
+                if constexpr (STOCHASTIC) {
+                    const uint64_t r = mix64(a.key + 8 * t.first_block + e / 4);
+                    const uint64_t backwards = (r << 48) | ((r << 16) & 0xFFFF00000000ull) | ((r >> 16) & 0xFFFF0000ull) | (r >> 48);
+                    mc = fp8_stochastic<false>(ym, r);
+                    vc = fp8_stochastic<true>(yv, backwards);
+                } else {
+                    mc = fp8_nearest<false>(ym);
+                    vc = fp8_nearest<true>(yv);
+                }
+                store_bytes(t.m + e, mc, count[k]);
+                store_bytes(t.v + e, vc, count[k]);
+                if ((threadIdx.x & 7) == 0 && (whole || i < left)) {
+                    ((uint8_t DSLLM_GLOBAL *)t.m_scale)[e / 32] = uint8_t(mb);
+                    ((uint8_t DSLLM_GLOBAL *)t.v_scale)[e / 32] = uint8_t(vb);
+                }
+            }
+            const f32x4 next = updated(w[k], m[k], v[k], keep, a);
+            store_upto4<CKPT_F32>(t.master + e, next, count[k]);
+            if constexpr (PARAM != 0) store_upto4<PARAM>(t.param + 2 * e, next, count[k]);
+        }
+    };
+    if (left >= kWave) work(std::true_type{});
+    else work(std::false_type{});
 }
 
 constexpr uint32_t kGradsALaunch = 448;
@@ -184,10 +257,15 @@ __global__ __launch_bounds__(kGradsALaunch) void set_grads_kernel(TensorEntry *t
 
 template <int GRAD, int PARAM>
 void launch_adamw(const ckpt_optim *o, const StepArgs &a, bool stochastic, hipStream_t stream) {
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(o->n_spans), dim3(256), 0, stream, o->dev_tensors, o->dev_spans, a); };
-    if (o->cfg.state_bits == 32) go(adamw_kernel<GRAD, PARAM, 32, false>);
-    else if (stochastic) go(adamw_kernel<GRAD, PARAM, 8, true>);
-    else go(adamw_kernel<GRAD, PARAM, 8, false>);
+    auto go = [&](auto kernel, unsigned groups, unsigned lds) {
+        for (uint32_t first = 0; first < o->n_spans; first += kSpansALaunch) {
+            const unsigned blocks = std::min(o->n_spans - first, kSpansALaunch) * (kSpan / 256 / groups);
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64), blocks > kFreeBlocks ? lds : 0, stream, o->dev_tensors, o->dev_spans + first, a);
+        }
+    };
+    if (o->cfg.state_bits == 32) go(adamw_kernel<GRAD, PARAM, 32, false, 1>, 1, 12800);
+    else if (stochastic) go(adamw_kernel<GRAD, PARAM, 8, true, 2>, 2, 8192);
+    else go(adamw_kernel<GRAD, PARAM, 8, false, 2>, 2, 8192);
 }
 template <int GRAD>
 void launch_adamw(const ckpt_optim *o, const StepArgs &a, bool stochastic, hipStream_t stream) {
@@ -323,14 +401,13 @@ int ckpt_optim_grad_norm(ckpt_optim *o, double max_norm, double grad_scale, ckpt
         DeviceRanges ranges;
         if (const char *why = ranges.wrong(dev_out, sizeof *dev_out)) return refuse(CKPT_EINVAL, std::string("dev_out: ") + why);
         if (uint64_t(dev_out) % 8) return refuse(CKPT_EINVAL, "dev_out must be 8-byte aligned");
-        const unsigned blocks = o->n_spans < 1 ? 1 : o->n_spans > kNormBlocks ? kNormBlocks : o->n_spans;
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream), o->dev_tensors, o->dev_spans, o->n_spans, o->dev_scratch, dev_out, max_norm, grad_scale);
+        auto go = [&](auto kernel, uint32_t threads, uint32_t most) {
+            hipLaunchKernelGGL(kernel, dim3(norm_blocks(o->n_spans, most)), dim3(threads), 0, static_cast<hipStream_t>(hip_stream), o->dev_tensors, o->dev_spans, o->n_spans, o->dev_scratch, dev_out, max_norm, grad_scale);
         };
         switch (o->cfg.grad_dtype) {
-            case CKPT_F32: go(norm_kernel<CKPT_F32>); break;
-            case CKPT_BF16: go(norm_kernel<CKPT_BF16>); break;
-            default: go(norm_kernel<CKPT_F16>);
+            case CKPT_F32: go(norm_kernel<CKPT_F32, 256>, 256, 512); break;
+            case CKPT_BF16: go(norm_kernel<CKPT_BF16, 512>, 512, 1024); break;
+            default: go(norm_kernel<CKPT_F16, 512>, 512, 1024);
         }
         return launched();
     });
