@@ -49,7 +49,7 @@ __device__ __forceinline__ f32x4 mfma_fp4(u32x4 a, u32x4 b, f32x4 c, uint32_t a_
 // Half h of a step takes piece 2 q + h in the lanes 16 q to 16 q + 15 (any order of K will do that both sides share): a lane's two scales of a step are
 // then neighbours, in the upper or the lower half of an aligned word.
 // LDS layout of the scales: of eight rows the first two steps' 16 bytes one behind the other, then the other two steps' (every other eight rows the other way round).
-__device__ __forceinline__ uint32_t rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
+[[maybe_unused]] __device__ __forceinline__ uint32_t rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
 
 template <int BM, int BN, int NW, int STAGES>
 struct StepLoader {

@@ -1,4 +1,7 @@
 // Conversion to block-scaled formats and back (include/ckpt_train.h).
+#include <algorithm>
+#include <type_traits>
+
 #include "train_util.hpp"
 
 using namespace dsllm;
@@ -17,64 +20,128 @@ struct RowArgs {
     uint64_t code_pitch, scale_pitch;
     uint64_t blocks;            // of a row, with those behind its end that are to be zero
     uint64_t key;
+    uint64_t pieces;            // of a row, a wave's work each
 };
 
-// Eight lanes a block of 32 elements of a row, four each.
+// A wave takes 1024 elements of a row in groups of 256, four elements a lane; eight lanes a block of 32. Bound by memory when rounding to nearest: 60 M f32 to 8 bits 48 us = 6.3 TB/s (one group
+// a wave: 57); 45 M bf16 to 4 bits 24 us, two groups 27. Stochastically 59 us: three 64-bit products for every four elements.
+constexpr uint32_t kGroups = 4, kRowPiece = 256 * kGroups;
 template <int SRC, int FORMAT, bool STOCHASTIC, bool NONZERO>
 __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
-    const uint64_t total = a.rows * a.blocks, per_row = (a.cols + 3) / 4;
-    for (uint64_t b = uint64_t(blockIdx.x) * 32 + threadIdx.x / 8; b < total; b += uint64_t(gridDim.x) * 32) {
-        const uint64_t row = b / a.blocks, block = b - row * a.blocks, col = 32 * block + 4 * (threadIdx.x & 7);
-        const uint32_t count = col < a.cols ? uint32_t(a.cols - col < 4 ? a.cols - col : 4) : 0;
-        const f32x4 x = load_upto4<SRC>(a.src + (row * a.ld + col) * sizeof(typename Element<SRC>::one), count);
-        const uint32_t byte = scale_byte<FORMAT>(most_of_8(magnitude_bits(x)));
-        const f32x4 y = x * inverse_scale(byte);
-        uint32_t codes;
-        if constexpr (STOCHASTIC) {
-            const uint64_t r = mix64(a.key + row * per_row + col / 4);
-            codes = FORMAT == CKPT_MXFP4 ? fp4_stochastic(y, r) : fp8_stochastic<NONZERO>(y, r);
-        } else {
-            codes = FORMAT == CKPT_MXFP4 ? fp4_nearest(y) : fp8_nearest<NONZERO>(y);
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t item = uint64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t row = item / a.pieces, first = (item - row * a.pieces) * kRowPiece;
+    if (row >= a.rows) return;
+    auto work = [&](auto whole) {
+        f32x4 x[kGroups];
+        uint32_t count[kGroups];
+#pragma unroll
+        for (int k = 0; k < int(kGroups); k++) {
+            const uint64_t col = first + 256 * k + 4 * lane;
+            count[k] = whole ? 4 : col < a.cols ? uint32_t(a.cols - col < 4 ? a.cols - col : 4) : 0;
+            x[k] = load_upto4<SRC>(a.src + (row * a.ld + col) * sizeof(typename Element<SRC>::one), count[k]);
         }
-        if (FORMAT == CKPT_MXFP4) {
-            if (count < 4) codes &= (1u << (4 * count)) - 1;
-            if (col / 2 < a.code_pitch) *(uint16_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = uint16_t(codes);
-        } else {
-            if (count < 4) codes &= (1u << (8 * count)) - 1;
-            if (col < a.code_pitch) store_bytes(a.codes + row * a.code_pitch + col, codes, uint32_t(a.code_pitch - col < 4 ? a.code_pitch - col : 4));
+#pragma unroll
+        for (int k = 0; k < int(kGroups); k++) {
+            const uint64_t col = first + 256 * k + 4 * lane;
+            const uint32_t byte = scale_byte<FORMAT>(most_of_8(magnitude_bits(x[k])));
+            const f32x4 y = x[k] * inverse_scale(byte);
+            uint32_t codes;
+            if constexpr (STOCHASTIC) {
+                const uint64_t r = mix64(a.key + row * ((a.cols + 3) / 4) + col / 4);
+                codes = FORMAT == CKPT_MXFP4 ? fp4_stochastic(y, r) : fp8_stochastic<NONZERO>(y, r);
+            } else {
+                codes = FORMAT == CKPT_MXFP4 ? fp4_nearest(y) : fp8_nearest<NONZERO>(y);
+            }
+            if (FORMAT == CKPT_MXFP4) {
+                if (count[k] < 4) codes &= (1u << (4 * count[k])) - 1;
+                if (col / 2 < a.code_pitch) *(uint16_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = uint16_t(codes);
+            } else {
+                if (count[k] < 4) codes &= (1u << (8 * count[k])) - 1;
+                if (col < a.code_pitch) store_bytes(a.codes + row * a.code_pitch + col, codes, uint32_t(a.code_pitch - col < 4 ? a.code_pitch - col : 4));
+            }
+            if ((lane & 7) == 0 && col / 32 < a.scale_pitch) ((uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32] = uint8_t(byte);
         }
-        if ((threadIdx.x & 7) == 0 && block < a.scale_pitch) a.scales[row * a.scale_pitch + block] = uint8_t(byte);
-    }
+    };
+    // a piece that ends inside the row has loads without conditions: all are under way before the first is waited for
+    if (first + kRowPiece <= a.cols) work(std::true_type{});
+    else work(std::false_type{});
 }
 
-// A thread a block of 32 elements of a column: row `col` of the transpose. Blocks behind the last row are zero.
-template <int SRC, bool STOCHASTIC>
-__global__ __launch_bounds__(256) void columns_kernel(RowArgs a) {      // rows, cols: of src; codes, scales: of its transpose
-    const uint64_t total = a.cols * a.blocks, per_row = (a.rows + 3) / 4;
-    for (uint64_t t = uint64_t(blockIdx.x) * 256 + threadIdx.x; t < total; t += uint64_t(gridDim.x) * 256) {
-        const uint64_t block = t / a.cols, col = t - block * a.cols, row = 32 * block;
-        f32x4 x[8];
+// A tile of 128 x 128 elements, to the columns' form and, with BY_ROW, to the rows' as well, 64 rows at a time: read once, 32 lanes a row, rounded by rows as it comes, put into LDS, and read
+// from there by columns while the other 64 rows are under way. In LDS the rows of the second 32 begin 32 words further round the banks: the 32 columns x 2 blocks of 32 rows that a wave reads at
+// once lie in 64 different ones. 45 M f32 to both forms 47 us = 4.8 TB/s (all 128 rows at a time, two blocks a unit instead of four: 52; by two kernels that each read src 100), bf16 37 us, f32
+// stochastically 73. Loads that stand under a condition, with the conversion to f32 beside them, are waited for one by one: bf16 took 83 us with them.
+struct TileArgs {
+    RowArgs by_row, by_col;      // by_col: rows, cols are src's; codes, scales its transpose's
+    uint32_t tiles_across;
+};
+template <int SRC, bool STOCHASTIC, bool BY_ROW>
+__global__ __launch_bounds__(256, 4) void tile_kernel(TileArgs p) {
+    constexpr uint32_t kBytes = sizeof(typename Element<SRC>::one);
+    __shared__ float tile[128 * 64 + 32];
+    const RowArgs &a = p.by_row, &c = p.by_col;
+    const uint64_t tile_row = blockIdx.x / p.tiles_across, row0 = 128 * tile_row, col0 = 128 * (blockIdx.x - tile_row * uint64_t(p.tiles_across));
+    const uint32_t across = threadIdx.x & 31, down = threadIdx.x >> 5;
+    const uint64_t col = col0 + 4 * across;
+    const uint32_t count = col < c.cols ? uint32_t(c.cols - col < 4 ? c.cols - col : 4) : 0;
+    const bool whole = row0 + 128 <= c.rows && col0 + 128 <= c.cols;      // loads without conditions: all are under way before the first is waited for
+    const uint8_t *src = c.src + ((row0 + down) * c.ld + col) * kBytes;
+    typename Element<SRC>::four x[8];
+    auto load = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint8_t *at = src + (64 * half + 8 * i) * c.ld * kBytes;
+            typedef typename Element<SRC>::four four_bytealigned __attribute__((aligned(1)));
+            if (whole) x[i] = __builtin_nontemporal_load((const four_bytealigned DSLLM_GLOBAL *)at);
+            else x[i] = __builtin_convertvector(load_upto4<SRC>(at, row0 + 64 * half + 8 * i + down < c.rows ? count : 0), typename Element<SRC>::four);
+        }
+    };
+    load(0);
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+        if (half) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t r = 8 * i + down;
+            const uint64_t row = row0 + 64 * half + r;
+            const f32x4 v = __builtin_convertvector(x[i], f32x4);
+            *reinterpret_cast<f32x4 *>(tile + 128 * r + 32 * (r >> 5) + 4 * across) = v;
+            if constexpr (BY_ROW) {
+                const uint32_t byte = scale_byte<CKPT_MXFP4>(most_of_8(magnitude_bits(v)));
+                const f32x4 y = v * inverse_scale(byte);
+                uint32_t codes = STOCHASTIC ? fp4_stochastic(y, mix64(a.key + row * ((a.cols + 3) / 4) + col / 4)) : fp4_nearest(y);
+                if (count < 4) codes &= (1u << (4 * count)) - 1;
+                if (row < a.rows) {
+                    if (col / 2 < a.code_pitch) *(uint16_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = uint16_t(codes);
+                    if ((across & 7) == 0 && col / 32 < a.scale_pitch) ((uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32] = uint8_t(byte);
+                }
+            }
+        }
+        if (half == 0) load(1);
+        __syncthreads();
+        const uint32_t of_rows = threadIdx.x & 1, of_cols = threadIdx.x >> 1;
+        const uint64_t first = row0 + 64 * half + 32 * of_rows, block = first / 32, out = col0 + of_cols;
+        f32x4 y[8];
         uint32_t most = 0;
 #pragma unroll
         for (int g = 0; g < 8; g++) {
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const uint64_t r = row + 4 * g + j;
-                x[g][j] = r < a.rows ? float(((const typename Element<SRC>::one DSLLM_GLOBAL *)a.src)[r * a.ld + col]) : 0.0f;
-            }
-            most = max(most, magnitude_bits(x[g]));
+            for (int j = 0; j < 4; j++) y[g][j] = tile[128 * (32 * of_rows + 4 * g + j) + 32 * of_rows + of_cols];
+            most = max(most, magnitude_bits(y[g]));
         }
+        if (out >= c.cols) continue;
         const uint32_t byte = scale_byte<CKPT_MXFP4>(most);
         u32x4 codes{0, 0, 0, 0};
 #pragma unroll
         for (int g = 0; g < 8; g++) {
-            const f32x4 y = x[g] * inverse_scale(byte);
-            uint32_t c = STOCHASTIC ? fp4_stochastic(y, mix64(a.key + col * per_row + row / 4 + g)) : fp4_nearest(y);
-            if (row + 4 * g + 4 > a.rows) c = row + 4 * g < a.rows ? c & ((1u << (4 * (a.rows - row - 4 * g))) - 1) : 0;
-            codes[g / 2] |= c << (16 * (g & 1));
+            const f32x4 v = y[g] * inverse_scale(byte);
+            uint32_t four = STOCHASTIC ? fp4_stochastic(v, mix64(c.key + out * ((c.rows + 3) / 4) + first / 4 + g)) : fp4_nearest(v);
+            if (!whole && first + 4 * g + 4 > c.rows) four = first + 4 * g < c.rows ? four & ((1u << (4 * (c.rows - first - 4 * g))) - 1) : 0;
+            codes[g / 2] |= four << (16 * (g & 1));
         }
-        if (16 * block < a.code_pitch) *(u32x4 DSLLM_GLOBAL *)(a.codes + col * a.code_pitch + 16 * block) = codes;
-        if (block < a.scale_pitch) a.scales[col * a.scale_pitch + block] = uint8_t(byte);
+        if (16 * block < c.code_pitch) *(u32x4 DSLLM_GLOBAL *)(c.codes + out * c.code_pitch + 16 * block) = codes;
+        if (block < c.scale_pitch) ((uint8_t DSLLM_GLOBAL *)c.scales)[out * c.scale_pitch + block] = uint8_t(byte);
     }
 }
 
@@ -82,25 +149,35 @@ struct ValueArgs {
     const uint8_t *codes, *scales;
     uint64_t code_pitch, scale_pitch, rows, cols, ld;
     uint8_t *dst;
+    uint64_t pieces;
 };
 
+// Eight elements a lane, 512 of a row a wave. Bound by memory: 45 M 4-bit values to bf16 17.3 us = 6.6 TB/s (more a lane is no faster).
+constexpr uint32_t kValuePiece = 512;
 template <int FORMAT, int DST>
 __global__ __launch_bounds__(256) void values_kernel(ValueArgs a) {
-    const uint64_t per_row = (a.cols + 3) / 4, total = a.rows * per_row;
-    for (uint64_t t = uint64_t(blockIdx.x) * 256 + threadIdx.x; t < total; t += uint64_t(gridDim.x) * 256) {
-        const uint64_t row = t / per_row, col = 4 * (t - row * per_row);
-        const uint32_t count = uint32_t(a.cols - col < 4 ? a.cols - col : 4);
-        const float scale = scale_value(a.scales[row * a.scale_pitch + col / 32]);
-        f32x4 v;
-        if constexpr (FORMAT == CKPT_MXFP4) v = fp4_values(*(const uint16_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2), scale);
-        else v = fp8_values(load_bytes(a.codes + row * a.code_pitch + col, count)) * scale;
-        store_upto4<DST>(a.dst + (row * a.ld + col) * sizeof(typename Element<DST>::one), v, count);
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t item = uint64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t row = item / a.pieces, col = (item - row * a.pieces) * kValuePiece + 8 * lane;
+    if (row >= a.rows || col >= a.cols) return;
+    const float scale = scale_value(((const uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32]);
+    uint32_t codes[2];
+    if constexpr (FORMAT == CKPT_MXFP4) {
+        codes[0] = *(const uint32_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2);
+        codes[1] = codes[0] >> 16;
+    } else {
+        codes[0] = load_bytes(a.codes + row * a.code_pitch + col, uint32_t(min(a.cols - col, uint64_t(4))));
+        codes[1] = col + 4 < a.cols ? load_bytes(a.codes + row * a.code_pitch + col + 4, uint32_t(min(a.cols - col - 4, uint64_t(4)))) : 0;
     }
-}
-
-unsigned grid_for(uint64_t items, unsigned per_block) {
-    const uint64_t blocks = (items + per_block - 1) / per_block, most = 1u << 20;
-    return unsigned(blocks < most ? blocks : most);
+    f32x4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; h++) v[h] = FORMAT == CKPT_MXFP4 ? fp4_values(codes[h], scale) : fp8_values(codes[h]) * scale;
+    uint8_t *at = a.dst + (row * a.ld + col) * sizeof(typename Element<DST>::one);
+    if (col + 8 <= a.cols) store8<DST>(at, v[0], v[1]);
+    else {
+        store_upto4<DST>(at, v[0], uint32_t(a.cols - col));
+        if (col + 4 < a.cols) store_upto4<DST>(at + 4 * sizeof(typename Element<DST>::one), v[1], uint32_t(a.cols - col - 4));
+    }
 }
 
 uint64_t zeroed_blocks(const ckpt_mx_matrix &m) {
@@ -108,19 +185,30 @@ uint64_t zeroed_blocks(const ckpt_mx_matrix &m) {
     return codes > m.scale_pitch ? codes : m.scale_pitch;
 }
 
+// Returns false if the grid would have 2^32 work-items or more.
+bool fits_grid(uint64_t blocks) { return blocks < 1u << 24; }
+
 template <int SRC>
-void launch_quantize(const RowArgs &rows, const RowArgs &cols, int format, bool by_row, bool by_col, int rounding, hipStream_t stream) {
+bool launch_quantize(RowArgs rows, RowArgs cols, int format, bool by_row, bool by_col, int rounding, hipStream_t stream) {
     const bool stochastic = rounding & CKPT_ROUND_STOCHASTIC, nonzero = rounding & CKPT_ROUND_NONZERO;
-    if (by_row) {
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid_for(rows.rows * rows.blocks, 32)), dim3(256), 0, stream, rows); };
-        if (format == CKPT_MXFP4) stochastic ? go(rows_kernel<SRC, CKPT_MXFP4, true, false>) : go(rows_kernel<SRC, CKPT_MXFP4, false, false>);
-        else if (nonzero) stochastic ? go(rows_kernel<SRC, CKPT_MXFP8, true, true>) : go(rows_kernel<SRC, CKPT_MXFP8, false, true>);
-        else stochastic ? go(rows_kernel<SRC, CKPT_MXFP8, true, false>) : go(rows_kernel<SRC, CKPT_MXFP8, false, false>);
-    }
     if (by_col) {
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid_for(cols.cols * cols.blocks, 256)), dim3(256), 0, stream, cols); };
-        stochastic ? go(columns_kernel<SRC, true>) : go(columns_kernel<SRC, false>);
+        const uint64_t across = ((by_row ? std::max(rows.cols, 32 * rows.blocks) : cols.cols) + 127) / 128, down = (std::max(cols.rows, 32 * cols.blocks) + 127) / 128;
+        if (!fits_grid(across) || !fits_grid(down) || !fits_grid(across * down)) return false;
+        const TileArgs p{rows, cols, uint32_t(across)};
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(across * down)), dim3(256), 0, stream, p); };
+        if (by_row) stochastic ? go(tile_kernel<SRC, true, true>) : go(tile_kernel<SRC, false, true>);
+        else stochastic ? go(tile_kernel<SRC, true, false>) : go(tile_kernel<SRC, false, false>);
+        return true;
     }
+    auto go = [&](auto kernel) {
+        rows.pieces = (32 * rows.blocks + kRowPiece - 1) / kRowPiece;
+        if (rows.pieces > 1ull << 30 || rows.rows > 1ull << 32 || !fits_grid((rows.rows * rows.pieces + 3) / 4)) return false;
+        hipLaunchKernelGGL(kernel, dim3(unsigned((rows.rows * rows.pieces + 3) / 4)), dim3(256), 0, stream, rows);
+        return true;
+    };
+    if (format == CKPT_MXFP4) return stochastic ? go(rows_kernel<SRC, CKPT_MXFP4, true, false>) : go(rows_kernel<SRC, CKPT_MXFP4, false, false>);
+    if (nonzero) return stochastic ? go(rows_kernel<SRC, CKPT_MXFP8, true, true>) : go(rows_kernel<SRC, CKPT_MXFP8, false, true>);
+    return stochastic ? go(rows_kernel<SRC, CKPT_MXFP8, true, false>) : go(rows_kernel<SRC, CKPT_MXFP8, false, false>);
 }
 
 int quantize(const void *src, int32_t dtype, int64_t ld, const ckpt_mx_matrix *by_row, const ckpt_mx_matrix *by_col, int32_t rounding, uint64_t seed, hipStream_t stream) {
@@ -141,7 +229,7 @@ int quantize(const void *src, int32_t dtype, int64_t ld, const ckpt_mx_matrix *b
     if (ld < cols || ld > (1ll << 48) / rows) return refuse(CKPT_EINVAL, "ld is smaller than a row, or the matrix too large");
     if (uint64_t(src) % bytes) return refuse(CKPT_EINVAL, "src is not aligned to its element");
     if (const char *why = ranges.wrong(src, (uint64_t(rows - 1) * ld + cols) * bytes)) return refuse(CKPT_EINVAL, std::string("src: ") + why);
-    RowArgs r{static_cast<const uint8_t *>(src), uint64_t(ld), uint64_t(rows), uint64_t(cols), nullptr, nullptr, 0, 0, 0, 0}, c = r;
+    RowArgs r{static_cast<const uint8_t *>(src), uint64_t(ld), uint64_t(rows), uint64_t(cols), nullptr, nullptr, 0, 0, 0, 0, 0}, c = r;
     auto fill = [](RowArgs &a, const ckpt_mx_matrix *m, uint64_t key) {
         if (!m) return;
         a.codes = static_cast<uint8_t *>(m->codes);
@@ -154,11 +242,13 @@ int quantize(const void *src, int32_t dtype, int64_t ld, const ckpt_mx_matrix *b
     fill(r, by_row, mix64(seed));
     fill(c, by_col, mix64(~seed));
     const int format = by_row ? by_row->format : CKPT_MXFP4;
+    bool fits;
     switch (dtype) {
-        case CKPT_F32: launch_quantize<CKPT_F32>(r, c, format, by_row, by_col, rounding, stream); break;
-        case CKPT_BF16: launch_quantize<CKPT_BF16>(r, c, format, by_row, by_col, rounding, stream); break;
-        default: launch_quantize<CKPT_F16>(r, c, format, by_row, by_col, rounding, stream);
+        case CKPT_F32: fits = launch_quantize<CKPT_F32>(r, c, format, by_row, by_col, rounding, stream); break;
+        case CKPT_BF16: fits = launch_quantize<CKPT_BF16>(r, c, format, by_row, by_col, rounding, stream); break;
+        default: fits = launch_quantize<CKPT_F16>(r, c, format, by_row, by_col, rounding, stream);
     }
+    if (!fits) return refuse(CKPT_EINVAL, "the matrix takes more than 2^24 blocks of threads");
     return launched();
 }
 
@@ -172,9 +262,11 @@ int dequantize(const ckpt_mx_matrix *m, void *dst, int32_t dtype, int64_t ld, hi
     if (ld < m->cols || ld > (1ll << 48) / m->rows) return refuse(CKPT_EINVAL, "ld is smaller than a row, or the matrix too large");
     if (uint64_t(dst) % bytes) return refuse(CKPT_EINVAL, "dst is not aligned to its element");
     if (const char *why = ranges.wrong(dst, (uint64_t(m->rows - 1) * ld + m->cols) * bytes)) return refuse(CKPT_EINVAL, std::string("dst: ") + why);
-    const ValueArgs a{static_cast<const uint8_t *>(m->codes), static_cast<const uint8_t *>(m->scales), m->code_pitch, m->scale_pitch,
-                      uint64_t(m->rows), uint64_t(m->cols), uint64_t(ld), static_cast<uint8_t *>(dst)};
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid_for(a.rows * ((a.cols + 3) / 4), 256)), dim3(256), 0, stream, a); };
+    ValueArgs a{static_cast<const uint8_t *>(m->codes), static_cast<const uint8_t *>(m->scales), m->code_pitch, m->scale_pitch,
+                uint64_t(m->rows), uint64_t(m->cols), uint64_t(ld), static_cast<uint8_t *>(dst), 0};
+    a.pieces = (a.cols + kValuePiece - 1) / kValuePiece;
+    if (a.rows > 1ull << 32 || a.pieces > 1ull << 30 || !fits_grid((a.rows * a.pieces + 3) / 4)) return refuse(CKPT_EINVAL, "the matrix takes more than 2^24 blocks of threads");
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((a.rows * a.pieces + 3) / 4)), dim3(256), 0, stream, a); };
     const bool four = m->format == CKPT_MXFP4;
     switch (dtype) {
         case CKPT_F32: four ? go(values_kernel<CKPT_MXFP4, CKPT_F32>) : go(values_kernel<CKPT_MXFP8, CKPT_F32>); break;

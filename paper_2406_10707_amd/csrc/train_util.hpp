@@ -94,6 +94,18 @@ __device__ __forceinline__ void store4(void *p, f32x4 v) {
     typedef typename Element<DTYPE>::four four_bytealigned __attribute__((aligned(1)));
     __builtin_nontemporal_store(__builtin_convertvector(v, typename Element<DTYPE>::four), (four_bytealigned DSLLM_GLOBAL *)p);
 }
+template <int DTYPE>
+__device__ __forceinline__ void store8(void *p, f32x4 lo, f32x4 hi) {
+    if constexpr (DTYPE == CKPT_F32) {
+        store4<DTYPE>(p, lo);
+        store4<DTYPE>(static_cast<float *>(p) + 4, hi);
+    } else {
+        typedef typename Element<DTYPE>::one eight __attribute__((ext_vector_type(8)));
+        typedef eight eight_bytealigned __attribute__((aligned(1)));
+        const typename Element<DTYPE>::four a = __builtin_convertvector(lo, typename Element<DTYPE>::four), b = __builtin_convertvector(hi, typename Element<DTYPE>::four);
+        __builtin_nontemporal_store(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), (eight_bytealigned DSLLM_GLOBAL *)p);
+    }
+}
 // The first `count` of them, 0 in the place of the others.
 template <int DTYPE>
 __device__ __forceinline__ f32x4 load_upto4(const void *p, uint32_t count) {
@@ -153,16 +165,18 @@ __device__ __forceinline__ uint32_t fp4_nearest(f32x4 y) {
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[2], y[3], 1.0f, 1);
     return r & 0xFFFFu;
 }
-// The grid's steps are 0.5 below 2, 1 below 4, 2 above. In units of 0.5 / 2^16 a value is an integer of twenty bits, and rounding is adding the
-// random bits at the step's place and cutting below it. NaN gives code 0 (its block's scale says NaN).
+// From 1 on a code is the upper bits of the f32 pattern, the 22 below are rounded away; smaller values are multiples of 0.5. Rounding is adding the random bits at the place of what
+// is cut off and cutting. NaN gives some code (its block's scale says NaN).
 __device__ __forceinline__ uint32_t fp4_stochastic(f32x4 y, uint64_t random) {
     uint32_t r = 0;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        const uint32_t halves = uint32_t(fabsf(y[j]) * 131072.0f);
-        const uint32_t s = (halves >= 4u << 16) + (halves >= 8u << 16);
-        const uint32_t code = ((halves + (field(random, j) << s)) >> (16 + s)) + 2 * s;
-        r |= (code | (__float_as_uint(y[j]) >> 31 << 3)) << (4 * j);
+        const float a = fabsf(y[j]);
+        const uint32_t bits = field(random, j);
+        const uint32_t normal = ((__float_as_uint(a) + (bits << 6)) >> 22) - 252u;
+        const uint32_t small = (uint32_t(fminf(a, 1.0f) * 131072.0f) + bits) >> 16;
+        const uint32_t code = a >= 1.0f ? normal : small;
+        r |= (code & 7u) << (4 * j) | (__float_as_uint(y[j]) >> 31) << (4 * j + 3);
     }
     return r;
 }
