@@ -57,7 +57,7 @@ int ckpt_mx_layout(int32_t format, int64_t rows, int64_t cols, ckpt_mx_matrix *o
 
 /* Rounds src, a row-major matrix of src_dtype (CKPT_F32, CKPT_BF16, CKPT_F16; aligned to its element) with `ld` elements from row
  * to row, to by_row (rows x cols, blocks along the columns) and / or by_col (the transpose: cols x rows, blocks along the
- * rows), in one pass over src. Either may be NULL. by_col takes MXFP4 only. Random bits: key = mix(seed) for by_row, mix(~seed) for
+ * rows), in one pass over src. Either may be NULL. by_col takes MXFP4 only, as does by_row beside it. Random bits: key = mix(seed) for by_row, mix(~seed) for
  * by_col. A product that contracts over the columns of src takes by_row, one that contracts over its rows by_col. */
 int ckpt_mx_quantize(const void *src, int32_t src_dtype, int64_t ld, const ckpt_mx_matrix *by_row, const ckpt_mx_matrix *by_col,
                      int32_t rounding, uint64_t seed, void *stream);
@@ -69,7 +69,7 @@ int ckpt_mx_dequantize(const ckpt_mx_matrix *src, void *dst, int32_t dst_dtype, 
  * elements from row to row. Accumulated in f32 on the matrix cores; one rounding at the end. A linear layer y = x W^T takes (x, W)
  * forward, (dy, W by columns) for dx and (dy by columns, x by columns) for dW. Some sizes split K among blocks and need
  * workspace: ckpt_mx_gemm_workspace bytes (16-byte aligned, contents do not matter, not shared by calls that may overlap);
- * with less (or NULL) the call runs unsplit. C must not overlap A, B or the workspace. */
+ * with less (or NULL) the call runs with fewer parts or unsplit. C must not overlap A, B or the workspace. */
 int ckpt_mx_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes);
 int ckpt_mx_gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t c_dtype, int64_t ldc, int32_t accumulate,
                  void *workspace, uint64_t workspace_bytes, void *stream);

@@ -3,6 +3,8 @@
 // v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 x 128 by 128 x 16 E2M1 values: lane l holds the 32 consecutive values (16 bytes) of row
 // l mod 16 that make up block l / 16 of the step, and that block's scale byte. A and B are both kept by rows along K, so both sides
 // are read the same way; the instruction applies the two scales of a block to its partial sum.
+#include <algorithm>
+
 #include "gemm_tile.hpp"
 #include "mx_gemm_forms.hpp"
 #include "train_util.hpp"
@@ -70,11 +72,11 @@ struct StepLoader {
         ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.a + row * p.a_pitch), 0, (last_a + 1) * uint32_t(p.a_pitch), 0x00020000);
         rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.b + col * p.b_pitch), 0, (last_b + 1) * uint32_t(p.b_pitch), 0x00020000);
         const uint32_t row0 = (lane >> 3) + 8 * wave, piece = lane & 7;
+        const uint32_t fa = rotated(((lane >> 4) & 3) | ((wave & 1) << 2)), fb = rotated(((lane >> 4) & 1) | ((wave & 3) << 1));      // f of row0, and of every 32nd row from it
 #pragma unroll
         for (int i = 0; i < LA + LB; i++) {
             const uint32_t r = row0 + 8 * NW * (i < LA ? i : i - LA);
-            const uint32_t f = rotated(i < LA ? (r >> 1) & 7 : ((r >> 1) & 1) | (((r >> 3) & 3) << 1));
-            off[i] = (i < LA ? min(r, last_a) * uint32_t(p.a_pitch) : min(r, last_b) * uint32_t(p.b_pitch)) + 16 * (piece ^ f);
+            off[i] = (i < LA ? min(r, last_a) * uint32_t(p.a_pitch) : min(r, last_b) * uint32_t(p.b_pitch)) + 16 * (piece ^ (i < LA ? fa : fb));
         }
 #pragma unroll
         for (int i = 0; i < PARTS; i++) {
@@ -129,22 +131,28 @@ __device__ __forceinline__ void store_eight(const GemmArgs &p, typename Element<
     }
 }
 
-// Eight consecutive columns of a row of a tile of C.
+// Eight consecutive columns of a row of a tile of C: 16 bytes in bf16, twice that in f32.
+template <int OUT> constexpr int kEights = OUT == CKPT_F32 ? 2 : 1;
+template <int OUT>
+__device__ __forceinline__ void load_eight_at(u32x4 *old, __amdgpu_buffer_rsrc_t c, uint32_t at, uint32_t uniform) {
+#pragma unroll
+    for (int i = 0; i < kEights<OUT>; i++) old[i] = __builtin_amdgcn_raw_buffer_load_b128(c, at + 16 * i, uniform, 0);
+}
 template <int OUT, bool ADD>
-__device__ __forceinline__ void store_eight_at(__amdgpu_buffer_rsrc_t c, uint32_t at, uint32_t uniform, f32x4 lo, f32x4 hi) {
+__device__ __forceinline__ void store_eight_at(__amdgpu_buffer_rsrc_t c, uint32_t at, uint32_t uniform, f32x4 lo, f32x4 hi, const u32x4 *old) {
     if constexpr (OUT == CKPT_F32) {
         if constexpr (ADD) {
-            lo += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(c, at, uniform, 0));
-            hi += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(c, at + 16, uniform, 0));
+            lo += __builtin_bit_cast(f32x4, old[0]);
+            hi += __builtin_bit_cast(f32x4, old[1]);
         }
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), c, at, uniform, 0);
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), c, at + 16, uniform, 0);
     } else {
         typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
         if constexpr (ADD) {
-            const bf16x8 old = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(c, at, uniform, 0));
-            lo += __builtin_convertvector(__builtin_shufflevector(old, old, 0, 1, 2, 3), f32x4);
-            hi += __builtin_convertvector(__builtin_shufflevector(old, old, 4, 5, 6, 7), f32x4);
+            const bf16x8 was = __builtin_bit_cast(bf16x8, old[0]);
+            lo += __builtin_convertvector(__builtin_shufflevector(was, was, 0, 1, 2, 3), f32x4);
+            hi += __builtin_convertvector(__builtin_shufflevector(was, was, 4, 5, 6, 7), f32x4);
         }
         const bf16x8 both = __builtin_shufflevector(__builtin_convertvector(lo, bf16x4), __builtin_convertvector(hi, bf16x4), 0, 1, 2, 3, 4, 5, 6, 7);
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, both), c, at, uniform, 0);
@@ -213,11 +221,6 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
             if (at(i) >= 2 * HALF + (i < TN ? 0 : TN * (i - TN)) - 1) return false;
         return true;
     }(shift_at), "scales are shifted before they count");
-    f32x4 acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; i++)
-#pragma unroll
-        for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0, 0, 0, 0};
     // Steps are counted from the part of K's first, which is a multiple of 4. Past the end the last step is loaded again, into a stage nothing reads.
     const uint32_t first = blockIdx.y * p.steps_a_split, steps = min(p.steps - first, p.steps_a_split), windows = first / 4;
     // load i of those that go out in step 4 window + turn: one of a later window of scales (not in every step), then the panels of the step STAGES later
@@ -234,6 +237,12 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
 #pragma unroll
         for (int i = 0; i < Loader::PANELS; i++) load.issue_panels(lds, s, first + min(uint32_t(s), steps - 1), i);
     }
+    __builtin_amdgcn_sched_barrier(0);      // the loads go out first
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0, 0, 0, 0};
     wait_loads_and_meet<(STAGES - 1) * Loader::PANELS + 1>();
 #pragma unroll
     for (int i = 0; i < FRAGS; i++) { read(0, 0, i); read_scale(0, 0, 0, i); }
@@ -312,15 +321,25 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
         const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(tile, 0, 0xFFFFFFFFu, 0x00020000);
         const uint32_t pitch = uint32_t(p.ldc) * sizeof(Out), lane_at = (wm * 16 * TM + ar) * pitch + (wn * 16 * TN + 8 * q) * sizeof(Out);
         auto store_tile = [&](auto add) {
+            constexpr int PAIRS = TN / 2, E = kEights<OUT>;
+            u32x4 old[2][PAIRS * E];      // what is there, a row of fragments ahead
+            auto load_row = [&](int i) {
 #pragma unroll
-            for (int i = 0; i < TM; i++)
+                for (int j = 0; j < PAIRS; j++) load_eight_at<OUT>(&old[i & 1][j * E], rc, lane_at + 32 * j * sizeof(Out), 16 * i * pitch);
+            };
+            if constexpr (add) load_row(0);
 #pragma unroll
-                for (int j = 0; j < TN; j += 2) {
+            for (int i = 0; i < TM; i++) {
+                if constexpr (add)
+                    if (i + 1 < TM) load_row(i + 1);
+#pragma unroll
+                for (int j = 0; j < PAIRS; j++) {
                     // in their registers up to here: copied out all at once they would spill
-                    if constexpr (NAMED) asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
-                    store_eight_at<OUT, add>(rc, lane_at + 16 * j * sizeof(Out), 16 * i * pitch, acc[i][j], acc[i][j + 1]);
+                    if constexpr (NAMED) asm volatile("" : "+a"(acc[i][2 * j]), "+a"(acc[i][2 * j + 1]));
+                    store_eight_at<OUT, add>(rc, lane_at + 32 * j * sizeof(Out), 16 * i * pitch, acc[i][2 * j], acc[i][2 * j + 1], &old[i & 1][j * E]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+            }
         };
         if (p.accumulate) store_tile(std::true_type{});
         else store_tile(std::false_type{});
@@ -393,12 +412,28 @@ __global__ __launch_bounds__(256) void gemm_long_kernel(GemmArgs p) {
             }
 }
 
+// The parts' sums of a product whose K was split, added in order. Rows of the parts are `pitch` elements apart, a multiple of 4.
+template <int OUT>
+__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ parts, uint32_t splits, int64_t split, uint32_t pitch, GemmArgs p) {
+    const uint64_t t = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t quads = pitch / 4, row = uint32_t(t / quads), col = 4 * uint32_t(t - uint64_t(row) * quads);
+    if (row >= p.m) return;
+    const float *at = parts + int64_t(row) * pitch + col;
+    f32x4 sum = *(const f32x4 DSLLM_GLOBAL *)at;
+    for (uint32_t s = 1; s < splits; s++) sum += *(const f32x4 DSLLM_GLOBAL *)(at + s * split);
+    typedef typename Element<OUT>::one Out;
+    Out *c = static_cast<Out *>(p.c) + row * p.ldc + col;
+    const uint32_t count = uint32_t(min(p.n - col, int64_t(4)));
+    if (p.accumulate) sum += load_upto4<OUT>(c, count);
+    store_upto4<OUT>(c, sum, count);
+}
+
 // In the order of kMxGemmForms
 template <int OUT>
-void launch_form(int form, const GemmArgs &p, hipStream_t stream) {
+void launch_form(int form, uint32_t splits, const GemmArgs &p, hipStream_t stream) {
     const MxGemmForm &f = kMxGemmForms[form];
     const uint32_t tiles_m = uint32_t((p.m + f.bm - 1) / f.bm), tiles_n = uint32_t((p.n + f.bn - 1) / f.bn);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n), dim3(256), 0, stream, p, TileOrder(tiles_m, tiles_n, true)); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n, splits), dim3(256), 0, stream, p, TileOrder(tiles_m, tiles_n, true)); };
     switch (form) {
         case 0: go(gemm_tile_kernel<1, 2, 2, 8, 8, 2, 2, 4, OUT>); break;
         case 1: go(gemm_tile_kernel<1, 2, 2, 6, 6, 2, 1, 3, OUT>); break;
@@ -425,16 +460,34 @@ int gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t dtyp
     if (ldc < n || ldc > (1ll << 48) / m) return refuse(CKPT_EINVAL, "ldc is smaller than a row, or C too large");
     if (uint64_t(c) % bytes) return refuse(CKPT_EINVAL, "C is not aligned to its element");
     if (const char *why = ranges.wrong(c, (uint64_t(m - 1) * ldc + n) * bytes)) return refuse(CKPT_EINVAL, std::string("C: ") + why);
-    (void)workspace; (void)workspace_bytes;
     const bool vector = uint64_t(c) % 16 == 0 && ldc * bytes % 16 == 0 && ldc <= 1 << 21;      // 256 rows in 32-bit offsets
     const uint32_t steps = uint32_t((k + 255) / 256);
     GemmArgs p{static_cast<const uint8_t *>(a->codes), static_cast<const uint8_t *>(b->codes), static_cast<const uint8_t *>(a->scales), static_cast<const uint8_t *>(b->scales),
                a->code_pitch, b->code_pitch, a->scale_pitch, b->scale_pitch, c, ldc, m, n, steps, steps, 0, accumulate, vector};
-    const int form = steps && a->code_pitch <= 1u << 23 && b->code_pitch <= 1u << 23 && a->scale_pitch <= 1u << 23 && b->scale_pitch <= 1u << 23
-                         ? mx_gemm_form(uint64_t(m), uint64_t(n), uint64_t(k), dtype == CKPT_F32) : -1;
-    if (form >= 0) {
-        if (dtype == CKPT_F32) launch_form<CKPT_F32>(form, p, stream);
-        else launch_form<CKPT_BF16>(form, p, stream);
+    const bool loadable = a->code_pitch <= 1u << 23 && b->code_pitch <= 1u << 23 && a->scale_pitch <= 1u << 23 && b->scale_pitch <= 1u << 23;
+    MxGemmChoice choice = steps && loadable ? mx_gemm_choice(uint64_t(m), uint64_t(n), uint64_t(k), dtype == CKPT_F32, workspace ? workspace_bytes : 0) : MxGemmChoice{-1, 1};
+    if (choice.splits > 1) {
+        const uint64_t bytes_needed = mx_gemm_part_bytes(uint64_t(m), uint64_t(n)) * choice.splits;
+        if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
+        if (const char *why = ranges.wrong(workspace, bytes_needed)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
+        const uint32_t pitch = uint32_t(mx_gemm_part_pitch(uint64_t(n)));
+        GemmArgs parts = p;
+        parts.c = workspace;
+        parts.ldc = pitch;
+        parts.accumulate = 0;
+        parts.vector = pitch <= 1 << 21;
+        parts.c_split = m * pitch;
+        parts.steps_a_split = mx_gemm_steps_a_split(steps, choice.splits);
+        launch_form<CKPT_F32>(choice.form, choice.splits, parts, stream);
+        const uint64_t threads = uint64_t(m) * (pitch / 4);
+        auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((threads + 255) / 256)), dim3(256), 0, stream, static_cast<const float *>(workspace), choice.splits, parts.c_split, pitch, p); };
+        if (dtype == CKPT_F32) join(join_kernel<CKPT_F32>);
+        else join(join_kernel<CKPT_BF16>);
+        return launched();
+    }
+    if (choice.form >= 0) {
+        if (dtype == CKPT_F32) launch_form<CKPT_F32>(choice.form, 1, p, stream);
+        else launch_form<CKPT_BF16>(choice.form, 1, p, stream);
         return launched();
     }
     const dim3 grid(unsigned((n + 63) / 64), unsigned((m + 63) / 64));
@@ -452,6 +505,12 @@ int ckpt_mx_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes) {
     return at_c_entry([&] {
         if (!bytes || m < 0 || n < 0 || k < 0) return refuse(CKPT_EINVAL, "null argument or negative size");
         *bytes = 0;
+        if (m > 0x7FFFFFFF || n > 0x7FFFFFFF || k > 0x7FFFFFFF) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1");
+        if (!m || !n || !k) return int(CKPT_OK);
+        for (bool f32 : {false, true}) {
+            const MxGemmChoice c = mx_gemm_choice(uint64_t(m), uint64_t(n), uint64_t(k), f32, UINT64_MAX);
+            if (c.splits > 1) *bytes = std::max(*bytes, mx_gemm_part_bytes(uint64_t(m), uint64_t(n)) * c.splits);
+        }
         return int(CKPT_OK);
     });
 }

@@ -24,24 +24,39 @@ constexpr MxGemmForm kMxGemmForms[] = {
 };
 constexpr int kMxGemmFormCount = sizeof(kMxGemmForms) / sizeof(kMxGemmForms[0]);
 constexpr uint32_t kComputeUnits = 256;
+constexpr double kJoin = 4.5, kJoinBytes = 5e6;      // us; bytes a us
 
-inline double mx_gemm_cost(const MxGemmForm &f, uint64_t m, uint64_t n, uint64_t k, bool f32_out) {
-    const uint64_t tiles = f.tiles(m, n), at_once = kComputeUnits * f.together, full = tiles / at_once, rest = tiles % at_once;
-    const double steps = double((k + 255) / 256), block = f.block * (f32_out ? 1.3 : 1.0);
-    double t = double(full) * (steps * f.step[f.together - 1] + block);
-    if (rest) t += steps * f.step[(rest + kComputeUnits - 1) / kComputeUnits - 1] + block;
+// `splits` blocks share a tile, each with a part of K.
+inline double mx_gemm_cost(const MxGemmForm &f, uint64_t m, uint64_t n, uint64_t steps, uint32_t splits, bool f32_out) {
+    const uint64_t blocks = f.tiles(m, n) * splits, at_once = kComputeUnits * f.together, full = blocks / at_once, rest = blocks % at_once;
+    const double block = f.block * (f32_out || splits > 1 ? 1.3 : 1.0);
+    double t = double(full) * (double(steps) * f.step[f.together - 1] + block);
+    if (rest) t += double(steps) * f.step[(rest + kComputeUnits - 1) / kComputeUnits - 1] + block;
     return t;
 }
 
-// The cheapest whose grid has fewer than 2^32 work-items; -1 if there is none.
-inline int mx_gemm_form(uint64_t m, uint64_t n, uint64_t k, bool f32_out) {
-    int best = -1;
+// Parts of K lie one behind the other in the workspace, as f32 rows of whole 16 bytes; each has a multiple of four steps (a window of scales).
+inline uint64_t mx_gemm_part_pitch(uint64_t n) { return (n + 3) / 4 * 4; }
+inline uint64_t mx_gemm_part_bytes(uint64_t m, uint64_t n) { return m * mx_gemm_part_pitch(n) * 4; }
+inline uint32_t mx_gemm_steps_a_split(uint32_t steps, uint32_t splits) { return ((steps + splits - 1) / splits + 3) / 4 * 4; }
+
+struct MxGemmChoice { int form; uint32_t splits; };
+
+// The cheapest form and number of parts whose grid has fewer than 2^32 work-items and whose parts fit the workspace; form -1 if there is none. Joining the parts costs another launch and
+// the way of the parts to memory and back.
+inline MxGemmChoice mx_gemm_choice(uint64_t m, uint64_t n, uint64_t k, bool f32_out, uint64_t workspace) {
+    const uint32_t steps = uint32_t((k + 255) / 256);
+    MxGemmChoice best{-1, 1};
     double least = 0;
-    for (int f = 0; f < kMxGemmFormCount; f++) {
-        if (kMxGemmForms[f].tiles(m, n) >= 1u << 24) continue;
-        const double t = mx_gemm_cost(kMxGemmForms[f], m, n, k, f32_out);
-        if (best < 0 || t < least) { best = f; least = t; }
-    }
+    for (int f = 0; f < kMxGemmFormCount; f++)
+        for (uint32_t splits = 1; splits <= 16; splits *= 2) {
+            const uint32_t each = mx_gemm_steps_a_split(steps, splits);
+            if (splits > 1 && (uint64_t(each) * (splits - 1) >= steps || mx_gemm_part_bytes(m, n) > workspace / splits)) break;
+            if (kMxGemmForms[f].tiles(m, n) * splits >= 1u << 24) break;
+            double t = mx_gemm_cost(kMxGemmForms[f], m, n, splits > 1 ? each : steps, splits, f32_out);
+            if (splits > 1) t += kJoin + double(mx_gemm_part_bytes(m, n)) * (2 * splits + 1) / kJoinBytes;
+            if (best.form < 0 || t < least) { best = MxGemmChoice{f, splits}; least = t; }
+        }
     return best;
 }
 

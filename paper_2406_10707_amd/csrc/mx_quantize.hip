@@ -221,6 +221,7 @@ int quantize(const void *src, int32_t dtype, int64_t ld, const ckpt_mx_matrix *b
         if (m)
             if (const char *why = wrong_mx_matrix(m, ranges)) return refuse(CKPT_EINVAL, std::string(m == by_row ? "by_row: " : "by_col: ") + why);
     if (by_col && by_col->format != CKPT_MXFP4) return refuse(CKPT_EINVAL, "by_col: only CKPT_MXFP4");
+    if (by_col && by_row && by_row->format != CKPT_MXFP4) return refuse(CKPT_EINVAL, "by_row: only CKPT_MXFP4 beside by_col");
     if (by_row && by_row->format == CKPT_MXFP4 && (rounding & CKPT_ROUND_NONZERO)) return refuse(CKPT_EINVAL, "CKPT_ROUND_NONZERO is for CKPT_MXFP8");
     if (by_col && (rounding & CKPT_ROUND_NONZERO)) return refuse(CKPT_EINVAL, "CKPT_ROUND_NONZERO is for CKPT_MXFP8");
     if (by_row && by_col && (by_row->rows != by_col->cols || by_row->cols != by_col->rows)) return refuse(CKPT_EINVAL, "by_col is not of the transpose's size");

@@ -7,6 +7,7 @@ import pytest
 from oracle import train_oracle as to
 from paper_2406_10707_amd import binding as B
 from paper_2406_10707_amd import harness
+from tests import gpu_util as gu
 from tests.test_gpu_train_mx import content, guarded
 
 pytestmark = pytest.mark.gpu
@@ -73,6 +74,49 @@ def test_products_are_exact(out, accumulate):
         assert magnitude.max() + 64 < 2.0 ** 22, "partial sums are multiples of 1/4 that 24 bits hold"
         got, before = product(a, b, m, n, kk, out, accumulate, (k % 3) * 5, rng, shift=k % 4)
         assert np.array_equal(got, exactly(want + before if accumulate else want, out))
+
+
+@pytest.mark.parametrize("out,accumulate", [("bf16", True), ("f32", False)])
+@pytest.mark.parametrize("m,n,k", [(1, 64, 16384), (64, 512, 16384), (5, 70, 17000), (130, 100, 20000), (16, 1001, 16000)])
+def test_parts_of_a_long_axis(m, n, k, out, accumulate):
+    print(f"product {m} x {n} x {k} in parts", flush=True)
+    assert B.mx_gemm_workspace(m, n, k) > 0
+    rng = np.random.default_rng(6)
+    a, b = operand(m, k, rng, 0), operand(n, k, rng, 0)
+    want, magnitude = to.gemm(to.values(*a, to.MXFP4), to.values(*b, to.MXFP4))
+    assert magnitude.max() + 64 < 2.0 ** 22
+    got, before = product(a, b, m, n, k, out, accumulate, 3, rng, shift=1)
+    assert np.array_equal(got, exactly(want + before if accumulate else want, out))
+
+
+def test_offsets_beyond_32_bits():
+    """C of 70,000 x 70,000 bf16 is 9.8 GB; A and B are zero but for their last rows, and C is read where those meet."""
+    print("product with 9.8 GB of C", flush=True)
+    n, k, tail = 70000, 256, 48
+    rng = np.random.default_rng(8)
+    a, b = operand(tail, k, rng, 0), operand(tail, k, rng, 0)
+    mats, held = [], []
+    for codes, byte in (a, b):
+        cp, sp = B.mx_layout(to.MXFP4, n, k)
+        pc, ps = to.pack_rows(codes, byte, to.MXFP4, cp, sp)
+        c, s = harness.DevBuf(n * cp), harness.DevBuf(n * sp)
+        held += [c, s]
+        for buf, part, pitch in ((c, pc, cp), (s, ps, sp)):
+            B.proxy_device_fill_async(buf.ptr, 0, buf.nbytes, 0)
+            B.proxy_copy_h2d(buf.ptr + (n - tail) * pitch, part.ctypes.data, part.nbytes)
+        mats.append(B.mx_matrix(to.MXFP4, n, k, c.ptr, cp, s.ptr, sp))
+    c = harness.DevBuf(2 * n * n)
+    B.proxy_device_fill_async(c.ptr, 0xEE, c.nbytes, 0)
+    B.mx_gemm(mats[0], mats[1], c.ptr, B.CKPT_BF16, n, 0)
+    harness.synchronize()
+    want = exactly(to.gemm(to.values(*a, to.MXFP4), to.values(*b, to.MXFP4))[0], "bf16")
+    for i in range(tail):
+        row = to.half_values(gu.download(c, 2 * ((n - tail + i) * n), 2 * n).view(np.uint16), "bf16")
+        assert np.array_equal(row[n - tail:], want[i]) and not row[: n - tail].any()
+    for row in (0, 33333, n - tail - 1):
+        assert not to.half_values(gu.download(c, 2 * row * n, 2 * n).view(np.uint16), "bf16").any()
+    for buf in held + [c]:
+        buf.free()
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 64, 16384), (96, 96, 8192), (64, 200, 5000)])

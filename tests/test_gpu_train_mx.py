@@ -188,8 +188,55 @@ def test_what_is_refused():
         B.mx_quantize(src, B.CKPT_F32, 256, None, None, 0)
     with pytest.raises(B.CkptError):
         B.mx_quantize(src, B.CKPT_F32, 256, None, B.mx_matrix(B.CKPT_MXFP8, 64, 256, buf.ptr, 256, buf.ptr + 65536, 8), 0)
+    with pytest.raises(B.CkptError) as e:
+        B.mx_quantize(src, B.CKPT_F32, 256, B.mx_matrix(B.CKPT_MXFP8, 64, 256, buf.ptr, 256, buf.ptr + 65536, 8), B.mx_matrix(B.CKPT_MXFP4, 256, 64, buf.ptr, 128, buf.ptr + 65536, 16), 0)
+    assert "beside by_col" in e.value.text
     with pytest.raises(B.CkptError):
         B.mx_dequantize(B.mx_matrix(**good), src, B.CKPT_U8, 256, 0)
     with pytest.raises(B.CkptError):
         B.mx_layout(9, 1, 1)
     harness.synchronize()
+
+
+def test_offsets_beyond_32_bits():
+    """70,000 rows of 65,536 bf16 values are 9.2 GB, their codes 2.3 and 2.3; zeros but for the last rows and columns."""
+    print("quantise 9.2 GB by rows and by columns", flush=True)
+    rows, cols, tail = 70000, 65536, 40
+    src = harness.DevBuf(2 * rows * cols)
+    B.proxy_device_fill_async(src.ptr, 0, src.nbytes, 0)
+    stored, x = inputs(tail, cols, "bf16", 5, special=True)
+    B.proxy_copy_h2d(src.ptr + 2 * (rows - tail) * cols, stored.ctypes.data, stored.nbytes)
+    bufs, mats = [], []
+    for r, c in ((rows, cols), (cols, rows)):
+        cp, sp = B.mx_layout(to.MXFP4, r, c)
+        bufs.append((harness.DevBuf(r * cp), harness.DevBuf(r * sp), cp, sp))
+        mats.append(B.mx_matrix(to.MXFP4, r, c, bufs[-1][0].ptr, cp, bufs[-1][1].ptr, sp))
+    B.mx_quantize(src.ptr, B.CKPT_BF16, cols, mats[0], mats[1], 0)
+    harness.synchronize()
+    wc, ws = to.quantize(x, to.MXFP4)
+    codes, scales, cp, sp = bufs[0]
+    pc, ps = to.pack_rows(wc, ws, to.MXFP4, cp, sp)
+    assert np.array_equal(gu.download(scales, (rows - tail) * sp, tail * sp), ps.reshape(-1))
+    got = gu.download(codes, (rows - tail) * cp, tail * cp).reshape(tail, cp)
+    bad = np.repeat(ws == 255, 16, axis=1)
+    assert np.array_equal(got[:, : bad.shape[1]][~bad], pc[:, : bad.shape[1]][~bad])
+    assert not gu.download(codes, 0, 1 << 20).any() and not gu.download(scales, 0, 1 << 20).any()
+    codes, scales, cp, sp = bufs[1]
+    last = 64                                     # columns
+    y = np.zeros((last, rows))
+    y[:, rows - tail:] = x[:, cols - last:].T
+    wc, ws = to.quantize(y, to.MXFP4)
+    pc, ps = to.pack_rows(wc, ws, to.MXFP4, cp, sp)
+    assert np.array_equal(gu.download(scales, (cols - last) * sp, last * sp), ps.reshape(-1))
+    got = gu.download(codes, (cols - last) * cp, last * cp).reshape(last, cp)
+    bad = np.repeat(ws == 255, 16, axis=1)[:, :cp]
+    assert np.array_equal(got[:, : bad.shape[1]][~bad], pc[:, : bad.shape[1]][~bad])
+    values = harness.DevBuf(4 * rows * cols)
+    B.mx_dequantize(mats[0], values.ptr, B.CKPT_F32, cols, 0)
+    harness.synchronize()
+    wc, ws = to.quantize(x, to.MXFP4)
+    want = to.values(wc, ws, to.MXFP4)
+    got = gu.download(values, 4 * (rows - tail) * cols, 4 * tail * cols).view(np.float32).reshape(tail, cols)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~np.isnan(want)], want[~np.isnan(want)])
+    for b in [src, values] + [x for y in bufs for x in y[:2]]:
+        b.free()

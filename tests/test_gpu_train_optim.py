@@ -276,6 +276,61 @@ def test_the_moments_follow_differences_of_the_loss():
     assert loss(got) < loss(w64)
 
 
+def test_a_nonfinite_gradient_without_the_norm_spoils_its_block_alone():
+    print("infinity in a block", flush=True)
+    s = Setup([1000], "f32", "bf16", 8, seed=12)
+    at, _ = s.arena.parts[s.state[0]["index"]["grad"]]
+    x = np.array([np.inf], np.float32)
+    B.proxy_copy_h2d(s.arena.buf.ptr + at + 4 * 70, x.ctypes.data, 4)
+    hyper = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, step=3)
+    s.opt.step(0, **hyper)
+    harness.synchronize()
+    s.arena.fetch()
+    bad = np.zeros(32, bool)
+    bad[70 // 32] = True
+    for name in ("m", "v"):
+        assert np.array_equal(s.part(0, name + "_scale") == 255, bad)
+    w = s.part(0, "master").view(np.float32)
+    assert np.isnan(w[70]) and np.isfinite(np.delete(w, 70)).all()
+
+
+def test_offsets_beyond_32_bits():
+    """One tensor of 2^32 + 1000 elements with 8-bit moments, 34 GB, zeros but for its end: gradient, weights and moments there change, nothing else does."""
+    print("adamw of 4.3 G elements", flush=True)
+    n, tail = (1 << 32) + 1000, 1500
+    rng = np.random.default_rng(2)
+    g, w = as_grad(1e-3 * rng.standard_normal(tail), "bf16"), (0.02 * rng.standard_normal(tail)).astype(np.float32)
+    first = (n - tail) // 32 * 32
+    g, w = np.concatenate([np.zeros(n - tail - first, g.dtype), g]), np.concatenate([np.zeros(n - tail - first, w.dtype), w])
+    bufs = {"grad": harness.DevBuf(2 * n), "master": harness.DevBuf(4 * n), "m": harness.DevBuf(n), "v": harness.DevBuf(n),
+            "m_scale": harness.DevBuf(-(-n // 32)), "v_scale": harness.DevBuf(-(-n // 32))}
+    for b in bufs.values():
+        B.proxy_device_fill_async(b.ptr, 0, b.nbytes, 0)
+    B.proxy_copy_h2d(bufs["grad"].ptr + 2 * first, g.ctypes.data, g.nbytes)
+    B.proxy_copy_h2d(bufs["master"].ptr + 4 * first, w.ctypes.data, w.nbytes)
+    opt = B.Optimizer([dict(numel=n, weight_decay=0.1, **{k: b.ptr for k, b in bufs.items()})], grad_dtype=B.CKPT_BF16, param_dtype=0, state_bits=8)
+    norm = harness.DevBuf(24)
+    opt.grad_norm(norm.ptr, 0)
+    opt.step(0, step=1, lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, seed=3, stochastic=True, norm=norm.ptr)
+    harness.synchronize()
+    values = grad_values(g, "bf16")
+    total = float(np.sum(values.astype(np.float64) ** 2))
+    assert abs(B.ckpt_norm_result.from_buffer_copy(gu.download(norm).tobytes()).sum_squares - total) <= 1e-12 * total
+    m, v = to.moments(np.zeros_like(w), np.zeros_like(w), values, 1.0, 0.9, 0.95)
+    rm, rv = to.step_bits16(3, 1, first // 32, w.size)
+    for name, x, r in (("m", m, rm), ("v", v, rv)):
+        c, b = to.moment8(x, r, nonzero=name == "v")
+        assert np.array_equal(gu.download(bufs[name], first, w.size), c) and np.array_equal(gu.download(bufs[name + "_scale"], first // 32, b.size), b)
+        assert not gu.download(bufs[name], first - (1 << 20), 1 << 20).any()
+    want, update = to.adamw(w, m, v, 1e-3, 0.9, 0.95, 1e-8, 1, 0.1)
+    got = gu.download(bufs["master"], 4 * first, 4 * w.size).view(np.float32)
+    assert np.all(np.abs(got - want) <= 2.0 ** -22 * np.abs(w) + 2.0 ** -19 * update + 1e-38)
+    assert not gu.download(bufs["master"], 0, 1 << 20).any()
+    opt.destroy()
+    for b in bufs.values():
+        b.free()
+
+
 def test_what_is_refused():
     print("refusals", flush=True)
     buf, small = harness.DevBuf(1 << 16), harness.DevBuf(64)

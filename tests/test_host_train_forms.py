@@ -9,11 +9,11 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MAIN = """#include <cstdio>
 #include "mx_gemm_forms.hpp"
 int main() {
-    unsigned long long m, n, k, f32;
-    while (scanf("%llu %llu %llu %llu", &m, &n, &k, &f32) == 4) {
-        const int f = dsllm::mx_gemm_form(m, n, k, f32);
-        if (f < 0) { printf("none,0\\n"); continue; }
-        printf("%s,%llu\\n", dsllm::kMxGemmForms[f].name, (unsigned long long)dsllm::kMxGemmForms[f].tiles(m, n));
+    unsigned long long m, n, k, f32, ws;
+    while (scanf("%llu %llu %llu %llu %llu", &m, &n, &k, &f32, &ws) == 5) {
+        const dsllm::MxGemmChoice c = dsllm::mx_gemm_choice(m, n, k, f32, ws);
+        if (c.form < 0) { printf("none,0,0\\n"); continue; }
+        printf("%s,%llu,%u\\n", dsllm::kMxGemmForms[c.form].name, (unsigned long long)dsllm::kMxGemmForms[c.form].tiles(m, n), c.splits);
     }
 }
 """
@@ -27,18 +27,29 @@ def ask(tmp_path_factory):
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-I", os.path.join(ROOT, "paper_2406_10707_amd", "csrc"), "-o", exe, str(d / "main.cpp")], check=True)
 
     def f(shapes):
-        out = subprocess.run([exe], input="".join("%d %d %d %d\n" % s for s in shapes), capture_output=True, text=True, check=True).stdout
-        return [(x.rsplit(",", 1)[0], int(x.rsplit(",", 1)[1])) for x in out.splitlines()]
+        out = subprocess.run([exe], input="".join("%d %d %d %d %d\n" % (*s, 1 << 40)[:5] for s in shapes), capture_output=True, text=True, check=True).stdout
+        return [(name, int(tiles), int(splits)) for name, tiles, splits in (x.rsplit(",", 2) for x in out.splitlines())]
 
     return f
 
 
 def test_every_form_is_some_sizes(ask):
     sizes = [(8192, 8192, 8192, 0), (2048, 4096, 11008, 0), (2048, 2048, 2048, 0), (2304, 768, 8190, 1), (1, 11008, 4096, 0), (1000, 2304, 768, 0)]
-    assert [name for name, _ in ask(sizes)] == ["256x256", "192x192", "128x128", "64x128", "64x64 four stages", "64x64 two stages"]
+    assert [name for name, _, _ in ask(sizes)] == ["256x256", "192x192", "128x128", "64x128", "64x64 four stages", "64x64 two stages"]
 
 
 def test_grids_count_in_32_bits(ask):
     shapes = [(m, n, k, 1) for m in (1, 65, 1 << 20, (1 << 31) - 1) for n in (1, 64, 1 << 12, 1 << 16) for k in (1, 8192) if m * n <= 1 << 37]
-    for shape, (name, tiles) in zip(shapes, ask(shapes)):
-        assert name != "none" and tiles * 256 < 1 << 32, (shape, name)
+    for shape, (name, tiles, splits) in zip(shapes, ask(shapes)):
+        assert name != "none" and tiles * splits * 256 < 1 << 32, (shape, name)
+
+
+def test_long_axes_of_few_tiles_are_split_if_there_is_room(ask):
+    shapes = [(64, 512, 16384, 0), (1, 64, 16384, 1), (16, 4096, 16384, 0)]
+    for shape, (_, tiles, splits) in zip(shapes, ask(shapes)):
+        m, n, k, _ = shape
+        steps = -(-k // 256)
+        each = -(-(-(-steps // splits)) // 4) * 4
+        assert splits > 1 and each * (splits - 1) < steps, (shape, splits)      # no part without steps
+        need = splits * m * n * 4
+        assert ask([(*shape, need)])[0][2] == splits and ask([(*shape, need - 1)])[0][2] < splits and ask([(*shape, 0)])[0][2] == 1
