@@ -23,44 +23,63 @@ struct RowArgs {
     uint64_t pieces;            // of a row, a wave's work each
 };
 
-// A wave takes 1024 elements of a row in groups of 256, four elements a lane; eight lanes a block of 32. Bound by memory when rounding to nearest: 60 M f32 to 8 bits 48 us = 6.3 TB/s (one group
-// a wave: 57); 45 M bf16 to 4 bits 24 us, two groups 27. Stochastically 59 us: three 64-bit products for every four elements.
-constexpr uint32_t kGroups = 4, kRowPiece = 256 * kGroups;
+// E2M1 codes of eight values of a row (eight times four bits), a block of which lies in four neighbouring lanes; `byte` is its scale.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t fp4_codes_of_eight(f32x4 lo, f32x4 hi, uint64_t first_group_of_random, uint32_t *byte) {
+    *byte = scale_byte<CKPT_MXFP4>(most_of_4(max(magnitude_bits(lo), magnitude_bits(hi))));
+    const float inverse = inverse_scale(*byte);
+    lo *= inverse;
+    hi *= inverse;
+    if constexpr (STOCHASTIC) return fp4_stochastic(lo, mix64(first_group_of_random)) | fp4_stochastic(hi, mix64(first_group_of_random + 1)) << 16;
+    else return fp4_nearest(lo) | fp4_nearest(hi) << 16;
+}
+
+// A wave takes 1024 elements of a row in groups of 512, eight elements a lane; four lanes a block of 32.
+constexpr uint32_t kGroups = 2, kRowPiece = 512 * kGroups;
 template <int SRC, int FORMAT, bool STOCHASTIC, bool NONZERO>
 __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
+    constexpr uint32_t kBytes = sizeof(typename Element<SRC>::one);
     const uint32_t lane = threadIdx.x & 63;
     const uint64_t item = uint64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint64_t row = item / a.pieces, first = (item - row * a.pieces) * kRowPiece;
     if (row >= a.rows) return;
     auto work = [&](auto whole) {
-        f32x4 x[kGroups];
+        Eight<SRC> x[kGroups];
         uint32_t count[kGroups];
 #pragma unroll
         for (int k = 0; k < int(kGroups); k++) {
-            const uint64_t col = first + 256 * k + 4 * lane;
-            count[k] = whole ? 4 : col < a.cols ? uint32_t(a.cols - col < 4 ? a.cols - col : 4) : 0;
-            x[k] = load_upto4<SRC>(a.src + (row * a.ld + col) * sizeof(typename Element<SRC>::one), count[k]);
+            const uint64_t col = first + 512 * k + 8 * lane;
+            count[k] = whole ? 8 : col < a.cols ? uint32_t(min(a.cols - col, uint64_t(8))) : 0;
+            if constexpr (whole) x[k].load(a.src + (row * a.ld + col) * kBytes);
+            else x[k].load_upto(a.src + (row * a.ld + col) * kBytes, count[k]);
         }
 #pragma unroll
         for (int k = 0; k < int(kGroups); k++) {
-            const uint64_t col = first + 256 * k + 4 * lane;
-            const uint32_t byte = scale_byte<FORMAT>(most_of_8(magnitude_bits(x[k])));
-            const f32x4 y = x[k] * inverse_scale(byte);
-            uint32_t codes;
-            if constexpr (STOCHASTIC) {
-                const uint64_t r = mix64(a.key + row * ((a.cols + 3) / 4) + col / 4);
-                codes = FORMAT == CKPT_MXFP4 ? fp4_stochastic(y, r) : fp8_stochastic<NONZERO>(y, r);
+            const uint64_t col = first + 512 * k + 8 * lane, random = a.key + row * ((a.cols + 3) / 4) + col / 4;
+            f32x4 lo = __builtin_convertvector(x[k].lo, f32x4), hi = __builtin_convertvector(x[k].hi, f32x4);
+            uint32_t byte;
+            if constexpr (FORMAT == CKPT_MXFP4) {
+                uint32_t codes = fp4_codes_of_eight<STOCHASTIC>(lo, hi, random, &byte);
+                if (count[k] < 8) codes &= (1u << (4 * count[k])) - 1;
+                if (col / 2 < a.code_pitch) *(uint32_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = codes;
             } else {
-                codes = FORMAT == CKPT_MXFP4 ? fp4_nearest(y) : fp8_nearest<NONZERO>(y);
+                byte = scale_byte<CKPT_MXFP8>(most_of_4(max(magnitude_bits(lo), magnitude_bits(hi))));
+                lo *= inverse_scale(byte);
+                hi *= inverse_scale(byte);
+                const uint32_t c0 = STOCHASTIC ? fp8_stochastic<NONZERO>(lo, mix64(random)) : fp8_nearest<NONZERO>(lo);
+                const uint32_t c1 = STOCHASTIC ? fp8_stochastic<NONZERO>(hi, mix64(random + 1)) : fp8_nearest<NONZERO>(hi);
+                uint8_t *at = a.codes + row * a.code_pitch + col;
+                if (whole || count[k] == 8) {
+                    typedef u32x2 two_bytealigned __attribute__((aligned(1)));
+                    __builtin_nontemporal_store(u32x2{c0, c1}, (two_bytealigned DSLLM_GLOBAL *)at);
+                } else if (col < a.code_pitch) {      // what the row has behind its last element is zero
+                    const uint32_t room = uint32_t(min(a.code_pitch - col, uint64_t(8)));
+                    const uint64_t both = (uint64_t(c1) << 32 | c0) & ((1ull << (8 * count[k])) - 1);
+                    store_bytes(at, uint32_t(both), min(room, 4u));
+                    if (room > 4) store_bytes(at + 4, uint32_t(both >> 32), room - 4);
+                }
             }
-            if (FORMAT == CKPT_MXFP4) {
-                if (count[k] < 4) codes &= (1u << (4 * count[k])) - 1;
-                if (col / 2 < a.code_pitch) *(uint16_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = uint16_t(codes);
-            } else {
-                if (count[k] < 4) codes &= (1u << (8 * count[k])) - 1;
-                if (col < a.code_pitch) store_bytes(a.codes + row * a.code_pitch + col, codes, uint32_t(a.code_pitch - col < 4 ? a.code_pitch - col : 4));
-            }
-            if ((lane & 7) == 0 && col / 32 < a.scale_pitch) ((uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32] = uint8_t(byte);
+            if ((lane & 3) == 0 && col / 32 < a.scale_pitch) ((uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32] = uint8_t(byte);
         }
     };
     // a piece that ends inside the row has loads without conditions: all are under way before the first is waited for
@@ -68,7 +87,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
     else work(std::false_type{});
 }
 
-// A tile of 128 x 128 elements, to the columns' form and, with BY_ROW, to the rows' as well, 64 rows at a time: read once, 32 lanes a row, rounded by rows as it comes, put into LDS, and read
+// A tile of 128 x 128 elements, to the columns' form and, with BY_ROW, to the rows' as well, 64 rows at a time: read once, 16 lanes a row, rounded by rows as it comes, put into LDS, and read
 // from there by columns while the other 64 rows are under way. In LDS the rows of the second 32 begin 32 words further round the banks: the 32 columns x 2 blocks of 32 rows that a wave reads at
 // once lie in 64 different ones. 45 M f32 to both forms 47 us = 4.8 TB/s (all 128 rows at a time, two blocks a unit instead of four: 52; by two kernels that each read src 100), bf16 37 us, f32
 // stochastically 73. Loads that stand under a condition, with the conversion to f32 beside them, are waited for one by one: bf16 took 83 us with them.
@@ -82,19 +101,19 @@ __global__ __launch_bounds__(256, 4) void tile_kernel(TileArgs p) {
     __shared__ float tile[128 * 64 + 32];
     const RowArgs &a = p.by_row, &c = p.by_col;
     const uint64_t tile_row = blockIdx.x / p.tiles_across, row0 = 128 * tile_row, col0 = 128 * (blockIdx.x - tile_row * uint64_t(p.tiles_across));
-    const uint32_t across = threadIdx.x & 31, down = threadIdx.x >> 5;
-    const uint64_t col = col0 + 4 * across;
-    const uint32_t count = col < c.cols ? uint32_t(c.cols - col < 4 ? c.cols - col : 4) : 0;
+    const uint32_t across = threadIdx.x & 15, down = threadIdx.x >> 4;
+    const uint64_t col = col0 + 8 * across;
+    const uint32_t count = col < c.cols ? uint32_t(min(c.cols - col, uint64_t(8))) : 0;
     const bool whole = row0 + 128 <= c.rows && col0 + 128 <= c.cols;      // loads without conditions: all are under way before the first is waited for
     const uint8_t *src = c.src + ((row0 + down) * c.ld + col) * kBytes;
-    typename Element<SRC>::four x[8];
+    Eight<SRC> x[4];
     auto load = [&](int half) {
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const uint8_t *at = src + (64 * half + 8 * i) * c.ld * kBytes;
-            typedef typename Element<SRC>::four four_bytealigned __attribute__((aligned(1)));
-            if (whole) x[i] = __builtin_nontemporal_load((const four_bytealigned DSLLM_GLOBAL *)at);
-            else x[i] = __builtin_convertvector(load_upto4<SRC>(at, row0 + 64 * half + 8 * i + down < c.rows ? count : 0), typename Element<SRC>::four);
+            for (int i = 0; i < 4; i++) x[i].load(src + (64 * half + 16 * i) * c.ld * kBytes);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) x[i].load_upto(src + (64 * half + 16 * i) * c.ld * kBytes, row0 + 64 * half + 16 * i + down < c.rows ? count : 0);
         }
     };
     load(0);
@@ -102,19 +121,19 @@ __global__ __launch_bounds__(256, 4) void tile_kernel(TileArgs p) {
     for (int half = 0; half < 2; half++) {
         if (half) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const uint32_t r = 8 * i + down;
+        for (int i = 0; i < 4; i++) {
+            const uint32_t r = 16 * i + down;
             const uint64_t row = row0 + 64 * half + r;
-            const f32x4 v = __builtin_convertvector(x[i], f32x4);
-            *reinterpret_cast<f32x4 *>(tile + 128 * r + 32 * (r >> 5) + 4 * across) = v;
+            const f32x4 lo = __builtin_convertvector(x[i].lo, f32x4), hi = __builtin_convertvector(x[i].hi, f32x4);
+            float *at = tile + 128 * r + 32 * (r >> 5) + 8 * across;
+            *reinterpret_cast<f32x4 *>(at) = lo;
+            *reinterpret_cast<f32x4 *>(at + 4) = hi;
             if constexpr (BY_ROW) {
-                const uint32_t byte = scale_byte<CKPT_MXFP4>(most_of_8(magnitude_bits(v)));
-                const f32x4 y = v * inverse_scale(byte);
-                uint32_t codes = STOCHASTIC ? fp4_stochastic(y, mix64(a.key + row * ((a.cols + 3) / 4) + col / 4)) : fp4_nearest(y);
-                if (count < 4) codes &= (1u << (4 * count)) - 1;
+                uint32_t byte, codes = fp4_codes_of_eight<STOCHASTIC>(lo, hi, a.key + row * ((a.cols + 3) / 4) + col / 4, &byte);
+                if (count < 8) codes &= (1u << (4 * count)) - 1;
                 if (row < a.rows) {
-                    if (col / 2 < a.code_pitch) *(uint16_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = uint16_t(codes);
-                    if ((across & 7) == 0 && col / 32 < a.scale_pitch) ((uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32] = uint8_t(byte);
+                    if (col / 2 < a.code_pitch) *(uint32_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = codes;
+                    if ((across & 3) == 0 && col / 32 < a.scale_pitch) ((uint8_t DSLLM_GLOBAL *)a.scales)[row * a.scale_pitch + col / 32] = uint8_t(byte);
                 }
             }
         }

@@ -106,6 +106,31 @@ __device__ __forceinline__ void store8(void *p, f32x4 lo, f32x4 hi) {
         __builtin_nontemporal_store(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), (eight_bytealigned DSLLM_GLOBAL *)p);
     }
 }
+// Eight elements, as they are stored; 16 bytes an access.
+template <int DTYPE>
+struct Eight {
+    typename Element<DTYPE>::four lo, hi;
+    __device__ __forceinline__ void load(const void *p) {
+        if constexpr (DTYPE == CKPT_F32) {
+            typedef f32x4 four_bytealigned __attribute__((aligned(1)));
+            lo = ((const four_bytealigned DSLLM_GLOBAL *)p)[0];      // not as read once: each access takes half of every 32 bytes
+            hi = ((const four_bytealigned DSLLM_GLOBAL *)p)[1];
+        } else {
+            typedef typename Element<DTYPE>::one eight __attribute__((ext_vector_type(8)));
+            typedef eight eight_bytealigned __attribute__((aligned(1)));
+            const eight e = __builtin_nontemporal_load((const eight_bytealigned DSLLM_GLOBAL *)p);
+            lo = __builtin_shufflevector(e, e, 0, 1, 2, 3);
+            hi = __builtin_shufflevector(e, e, 4, 5, 6, 7);
+        }
+    }
+    // the first `count` of them, 0 in the place of the others
+    __device__ __forceinline__ void load_upto(const void *p, uint32_t count) {
+        if (count >= 8) return load(p);
+        typedef const typename Element<DTYPE>::one DSLLM_GLOBAL *Pointer;
+#pragma unroll
+        for (uint32_t j = 0; j < 8; j++) (j < 4 ? lo : hi)[j & 3] = j < count ? ((Pointer)p)[j] : typename Element<DTYPE>::one(0);
+    }
+};
 // The first `count` of them, 0 in the place of the others.
 template <int DTYPE>
 __device__ __forceinline__ f32x4 load_upto4(const void *p, uint32_t count) {
@@ -226,6 +251,11 @@ __device__ __forceinline__ uint32_t most_of_8(uint32_t v) {
     v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0xB1, 0xF, 0xF, true)));     // neighbours exchanged
     v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4E, 0xF, 0xF, true)));     // pairs exchanged
     return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x141, 0xF, 0xF, true)));  // the eight mirrored
+}
+// Of four neighbouring lanes
+__device__ __forceinline__ uint32_t most_of_4(uint32_t v) {
+    v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0xB1, 0xF, 0xF, true)));
+    return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4E, 0xF, 0xF, true)));
 }
 __device__ __forceinline__ uint32_t magnitude_bits(f32x4 v) {
     const uint32_t m = 0x7FFFFFFFu;
