@@ -4,6 +4,7 @@
 // l mod 16 that make up block l / 16 of the step, and that block's scale byte. A and B are both kept by rows along K, so both sides
 // are read the same way; the instruction applies the two scales of a block to its partial sum.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_tile.hpp"
 #include "mx_gemm_forms.hpp"
@@ -367,6 +368,93 @@ __global__ __launch_bounds__(256, TOGETHER) void gemm_tile_kernel(GemmArgs p, Ti
 #endif
 }
 
+// ------------------------------------------------------------------ up to sixteen rows of A
+
+// As single tokens give them: B is what has to be read, once, at the rate of memory. A block takes 16 rows of B; its WAVES waves take the windows of four steps in turn, each with LDS of its own, so that
+// none waits for another before the sums are added, in wave order. Four steps of B and A are under way a wave; a step's place is filled again as soon as it has been read. LDS layouts as above (16 rows
+// of B, 16 of A, whose last is repeated where there are fewer; in the scales' window rows 16 to 31 are A's). Addresses are 64-bit ones.
+//
+// One token, launched in a row: 16384 x 16384 26 us = 5.4 TB/s (64 x 64 tiles 31), 4096 x 16384 8.2 (tiles 15.2, in four parts 10.9), 11008 x 4096 5.9 with two waves (four 6.4, tiles 6.1); below that the
+// launches are what counts (4.5 us). Fragments read straight from memory took 33, 11.7 and 7.4: sixteen lines a request.
+template <int WAVES, int OUT>
+__global__ __launch_bounds__(64 * WAVES) void gemm_few_kernel(GemmArgs p) {
+    constexpr int STEP = 2 * 16 * 128, SCALES = 32 * 32, WAVE = 4 * STEP + 2 * SCALES;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[WAVES * WAVE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, ar = lane & 15;
+    uint8_t *mine = lds + wave * WAVE;
+    const int64_t n0 = int64_t(blockIdx.x) * 16;
+    const uint8_t *from[4];      // this lane's piece of the rows lane / 8 of B, those 8 further, and of A's
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int r = 8 * (i & 1) + (lane >> 3);
+        const uint32_t piece = 16 * ((lane & 7) ^ rotated((r >> 1) & 7));
+        from[i] = (i < 2 ? p.b + min(n0 + r, p.n - 1) * p.b_pitch : p.a + min(int64_t(r), p.m - 1) * p.a_pitch) + piece;
+    }
+    const int sr = 8 * (lane >> 4) + (lane & 7);
+    const uint8_t *scales_from = sr < 16 ? p.b_scale + min(n0 + sr, p.n - 1) * p.b_scale_pitch : p.a_scale + min(int64_t(sr - 16), p.m - 1) * p.a_scale_pitch;
+    const uint32_t scale_half = 16 * (((lane >> 3) ^ (lane >> 4)) & 1), last_scales = uint32_t(sr < 16 ? p.b_scale_pitch : p.a_scale_pitch) - 16;
+    auto issue_scales = [&](uint32_t window, uint32_t odd) {      // what a row has behind its end is not used, and not read
+        const uint8_t *at = scales_from + min(32 * window + scale_half, last_scales);
+        __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)at, (DSLLM_LDS void *)(mine + 4 * STEP + (odd & 1) * SCALES), 16, 0, 0);
+    };
+    auto issue_step = [&](uint32_t window, int s) {
+        const uint64_t at = 128 * uint64_t(min(4 * window + s, p.steps - 1));
+#pragma unroll
+        for (int i = 0; i < 4; i++) __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(from[i] + at), (DSLLM_LDS void *)(mine + s * STEP + 1024 * i), 16, 0, 0);
+    };
+    const int frag_at = ar * 128, swizzle = rotated((ar >> 1) & 7);
+    const int scale_at_b = (ar >> 3) * 256 + ((ar >> 3) & 1) * 128 + (ar & 7) * 16 + 4 * (q >> 1), scale_at_a = scale_at_b + 512;
+    const uint32_t down = 16 * (q & 1), windows = (p.steps + 3) / 4;
+    f32x4 acc = {};
+    auto do_window = [&](auto more, uint32_t window, uint32_t odd) {
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            // this step's loads have landed; those of the later ones, and what has been asked for of the next window, may be under way
+            if constexpr (more) { if (s == 0) asm volatile("s_waitcnt vmcnt(12)" ::: "memory"); else asm volatile("s_waitcnt vmcnt(13)" ::: "memory"); }
+            else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * (3 - s)) : "memory");
+            u32x4 fb[2], fa[2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                fb[h] = *reinterpret_cast<const u32x4 *>(mine + s * STEP + frag_at + 16 * ((2 * q + h) ^ swizzle));
+                fa[h] = *reinterpret_cast<const u32x4 *>(mine + s * STEP + 2048 + frag_at + 16 * ((2 * q + h) ^ swizzle));
+            }
+            const uint8_t *sc = mine + 4 * STEP + (odd & 1) * SCALES;
+            const int of_step = (s >> 1) * 128 + (s & 1) * 8;
+            uint32_t sb = *reinterpret_cast<const uint32_t *>(sc + (scale_at_b ^ of_step)), sa = *reinterpret_cast<const uint32_t *>(sc + (scale_at_a ^ of_step));
+            asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(fb[0]), "+v"(fb[1]), "+v"(fa[0]), "+v"(fa[1]), "+v"(sb), "+v"(sa)::"memory");
+            if constexpr (more) {
+                if (s == 0) issue_scales(window + WAVES, odd + 1);
+                issue_step(window + WAVES, s);
+            }
+            if (4 * window + s >= p.steps) continue;
+            acc = mfma_fp4<0>(fb[0], fa[0], acc, sb >> down, sa >> down);
+            acc = mfma_fp4<1>(fb[1], fa[1], acc, sb >> down, sa >> down);
+        }
+    };
+    if (uint32_t(wave) < windows) {
+        issue_scales(wave, 0);
+#pragma unroll
+        for (int s = 0; s < 4; s++) issue_step(wave, s);
+        uint32_t window = wave, odd = 0;
+        for (; window + WAVES < windows; window += WAVES, odd++) do_window(std::true_type{}, window, odd);
+        do_window(std::false_type{}, window, odd);
+    }
+    __syncthreads();
+    f32x4 *part = reinterpret_cast<f32x4 *>(lds);
+    if (wave > 0) part[(wave - 1) * 64 + lane] = acc;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; w++) acc += part[w * 64 + lane];
+    typedef typename Element<OUT>::one Out;
+    const int64_t first_col = n0 + 4 * q;
+    if (ar >= p.m || first_col >= p.n) return;
+    Out *c = static_cast<Out *>(p.c) + ar * p.ldc + first_col;
+    const uint32_t count = uint32_t(min(p.n - first_col, int64_t(4)));
+    if (p.accumulate) acc += load_upto4<OUT>(c, count);
+    store_upto4<OUT>(c, acc, count);
+}
+
 // For rows of more than 2^23 bytes, which the loads above cannot address: four waves compute 64 x 64, a wave 32 x 32, straight from memory with 64-bit addresses. Rows
 // past the end are the last row again, and not stored.
 template <int OUT>
@@ -410,6 +498,13 @@ __global__ __launch_bounds__(256) void gemm_long_kernel(GemmArgs p) {
                 Out DSLLM_GLOBAL *at = (Out DSLLM_GLOBAL *)p.c + r * p.ldc + c;
                 *at = Out(acc[i][j][e] + (p.accumulate ? float(*at) : 0.0f));
             }
+}
+
+template <int OUT>
+void launch_few(uint32_t waves, const GemmArgs &p, hipStream_t stream) {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((p.n + 15) / 16)), dim3(64 * waves), 0, stream, p); };
+    if (waves == 2) go(gemm_few_kernel<2, OUT>);
+    else go(gemm_few_kernel<4, OUT>);
 }
 
 // The parts' sums of a product whose K was split, added in order. Rows of the parts are `pitch` elements apart, a multiple of 4.
@@ -464,6 +559,11 @@ int gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t dtyp
     const uint32_t steps = uint32_t((k + 255) / 256);
     GemmArgs p{static_cast<const uint8_t *>(a->codes), static_cast<const uint8_t *>(b->codes), static_cast<const uint8_t *>(a->scales), static_cast<const uint8_t *>(b->scales),
                a->code_pitch, b->code_pitch, a->scale_pitch, b->scale_pitch, c, ldc, m, n, steps, steps, 0, accumulate, vector};
+    if (const uint32_t waves = steps ? mx_gemm_few_waves(uint64_t(m), steps) : 0) {
+        if (dtype == CKPT_F32) launch_few<CKPT_F32>(waves, p, stream);
+        else launch_few<CKPT_BF16>(waves, p, stream);
+        return launched();
+    }
     const bool loadable = a->code_pitch <= 1u << 23 && b->code_pitch <= 1u << 23 && a->scale_pitch <= 1u << 23 && b->scale_pitch <= 1u << 23;
     MxGemmChoice choice = steps && loadable ? mx_gemm_choice(uint64_t(m), uint64_t(n), uint64_t(k), dtype == CKPT_F32, workspace ? workspace_bytes : 0) : MxGemmChoice{-1, 1};
     if (choice.splits > 1) {
@@ -506,7 +606,7 @@ int ckpt_mx_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes) {
         if (!bytes || m < 0 || n < 0 || k < 0) return refuse(CKPT_EINVAL, "null argument or negative size");
         *bytes = 0;
         if (m > 0x7FFFFFFF || n > 0x7FFFFFFF || k > 0x7FFFFFFF) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1");
-        if (!m || !n || !k) return int(CKPT_OK);
+        if (!m || !n || !k || mx_gemm_few_waves(uint64_t(m), uint32_t((k + 255) / 256))) return int(CKPT_OK);
         for (bool f32 : {false, true}) {
             const MxGemmChoice c = mx_gemm_choice(uint64_t(m), uint64_t(n), uint64_t(k), f32, UINT64_MAX);
             if (c.splits > 1) *bytes = std::max(*bytes, mx_gemm_part_bytes(uint64_t(m), uint64_t(n)) * c.splits);

@@ -4,7 +4,7 @@
 
 namespace dsllm {
 
-// A form's tile, how many of its blocks share a compute unit, and what it costs in us, fitted to 20 products from 1 x 11008 x 4096 to 8192^3 (mean 0.4 % over the
+// A form's tile, how many of its blocks share a compute unit, and what it costs in us, fitted to 20 products from 300 x 300 x 300 to 8192^3 (mean 0.4 % over the
 // best form of each, at most 4 %): a step of 256 values of K with 1, 2, 3 blocks on the unit, and what a block takes besides.
 struct MxGemmForm {
     const char *name;
@@ -39,6 +39,10 @@ inline double mx_gemm_cost(const MxGemmForm &f, uint64_t m, uint64_t n, uint64_t
 inline uint64_t mx_gemm_part_pitch(uint64_t n) { return (n + 3) / 4 * 4; }
 inline uint64_t mx_gemm_part_bytes(uint64_t m, uint64_t n) { return m * mx_gemm_part_pitch(n) * 4; }
 inline uint32_t mx_gemm_steps_a_split(uint32_t steps, uint32_t splits) { return ((steps + splits - 1) / splits + 3) / 4 * 4; }
+
+// Up to sixteen rows of A have a kernel of their own: its waves for each 16 rows of B, 0 for other products. Two where K is up to 4096 (11008 x 4096 5.9 us, with four 6.4), else four (16384 x 16384
+// 26.2, with two 27.9, with eight 29.5).
+inline uint32_t mx_gemm_few_waves(uint64_t m, uint32_t steps) { return m > 16 ? 0 : steps <= 16 ? 2 : 4; }
 
 struct MxGemmChoice { int form; uint32_t splits; };
 

@@ -61,7 +61,8 @@ def exactly(want, out):
 SHAPES = [(1, 1, 1), (1, 16, 32), (1, 64, 128), (1, 65, 4096), (1, 1000, 4128), (2, 33, 100), (3, 128, 256), (7, 260, 513), (8, 300, 640), (15, 64, 1000), (16, 48, 2048), (17, 130, 129),
           (31, 257, 384), (32, 96, 4100), (33, 512, 512), (48, 100, 300), (63, 65, 1025), (64, 64, 64), (65, 1, 300), (100, 100, 100), (128, 128, 256), (129, 127, 255),
           (200, 768, 768), (256, 256, 512), (257, 255, 2049), (300, 1000, 1300), (1000, 257, 256), (513, 514, 515), (96, 2304, 8190), (640, 640, 384), (1030, 1040, 640),
-          (768, 96, 6000), (1, 4096, 16384), (4097, 3, 40)]
+          (768, 96, 6000), (1, 4096, 16384), (4097, 3, 40),
+          (1, 17, 1024), (3, 100, 1025), (9, 31, 2500), (16, 200, 4096), (16, 33, 4097), (2, 1000, 12300), (13, 64, 16640), (5, 70, 17000)]
 
 
 @pytest.mark.parametrize("out,accumulate", [("bf16", False), ("f32", False), ("f32", True), ("bf16", True)])
@@ -77,7 +78,7 @@ def test_products_are_exact(out, accumulate):
 
 
 @pytest.mark.parametrize("out,accumulate", [("bf16", True), ("f32", False)])
-@pytest.mark.parametrize("m,n,k", [(1, 64, 16384), (64, 512, 16384), (5, 70, 17000), (130, 100, 20000), (16, 1001, 16000)])
+@pytest.mark.parametrize("m,n,k", [(17, 64, 16384), (64, 512, 16384), (25, 70, 17000), (130, 100, 20000), (30, 1001, 16000)])
 def test_parts_of_a_long_axis(m, n, k, out, accumulate):
     print(f"product {m} x {n} x {k} in parts", flush=True)
     assert B.mx_gemm_workspace(m, n, k) > 0

@@ -34,7 +34,7 @@ def ask(tmp_path_factory):
 
 
 def test_every_form_is_some_sizes(ask):
-    sizes = [(8192, 8192, 8192, 0), (2048, 4096, 11008, 0), (2048, 2048, 2048, 0), (2304, 768, 8190, 1), (1, 11008, 4096, 0), (1000, 2304, 768, 0)]
+    sizes = [(8192, 8192, 8192, 0), (2048, 4096, 11008, 0), (2048, 2048, 2048, 0), (2304, 768, 8190, 1), (40, 11008, 4096, 0), (1000, 2304, 768, 0)]
     assert [name for name, _, _ in ask(sizes)] == ["256x256", "192x192", "128x128", "64x128", "64x64 four stages", "64x64 two stages"]
 
 
@@ -45,7 +45,7 @@ def test_grids_count_in_32_bits(ask):
 
 
 def test_long_axes_of_few_tiles_are_split_if_there_is_room(ask):
-    shapes = [(64, 512, 16384, 0), (1, 64, 16384, 1), (16, 4096, 16384, 0)]
+    shapes = [(64, 512, 16384, 0), (17, 64, 16384, 1), (30, 4096, 16384, 0)]
     for shape, (_, tiles, splits) in zip(shapes, ask(shapes)):
         m, n, k, _ = shape
         steps = -(-k // 256)
