@@ -81,15 +81,17 @@ struct StepLoader {
         }
 #pragma unroll
         for (int i = 0; i < PARTS; i++) {
-            const uint32_t group = (i * NW + wave) % GROUPS, r = 32 * group + 8 * (lane >> 4) + (lane & 7);      // rows of A, then of B
+            // rows of A, then of B; of each 32 of B first the sixteen of the pair's first fragment
+            const uint32_t group = (i * NW + wave) % GROUPS, place = 8 * (lane >> 4) + (lane & 7);
             const bool of_a = 32 * group < BM;
+            const uint32_t r = 32 * group + (of_a ? place : 8 * ((place & 15) >> 2) + (place & 3) + 4 * (place >> 4));
             scale_place[i] = STAGES * PANEL + 1024 * group;
             scale_off[i] = (of_a ? min(r, last_a) * uint32_t(p.a_scale_pitch) : min(r - BM, last_b) * uint32_t(p.b_scale_pitch)) + 16 * (((lane >> 3) ^ (lane >> 4)) & 1);
             const uint8_t *base = of_a ? p.a_scale + row * p.a_scale_pitch : p.b_scale + col * p.b_scale_pitch;
             rs[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), 0, of_a ? (last_a + 1) * uint32_t(p.a_scale_pitch) : (last_b + 1) * uint32_t(p.b_scale_pitch), 0x00020000);
         }
     }
-    // where a row's 16 bytes of the window's first two steps lie; those of the other two: that ^ 128
+    // where the 16 bytes of the window's first two steps of the row in place r lie; those of the other two: that ^ 128
     static __device__ __forceinline__ int scale_at(int r) { return STAGES * PANEL + (r >> 3) * 256 + ((r >> 3) & 1) * 128 + (r & 7) * 16; }
     // part of a window of scales (four steps), which goes to the place of even or odd ones; what the row has behind its end is not used
     __device__ __forceinline__ void issue_scales(uint8_t *lds, uint32_t window, uint32_t odd, int part) const {
@@ -194,7 +196,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
         at_a[h] = (16 * TM * wm + ar) * 128 + 16 * ((2 * q + h) ^ rotated((ar >> 1) & 7));
         at_b[h] = (BM + 16 * TN * wn + br) * 128 + 16 * ((2 * q + h) ^ rotated(((ar >> 1) & 1) | ((ar >> 2) << 1)));
     }
-    const int at_sa = Loader::scale_at(16 * TM * wm + ar) + 4 * (q >> 1), at_sb = Loader::scale_at(BM + 16 * TN * wn + br) + 4 * (q >> 1);
+    const int at_sa = Loader::scale_at(16 * TM * wm + ar) + 4 * (q >> 1), at_sb = Loader::scale_at(BM + 16 * TN * wn + ar) + 4 * (q >> 1);
     const uint32_t down = 16 * (q & 1);
     u32x4 frag[2][FRAGS];      // [half of the step]: B fragments first, then A
     uint32_t scale[2][FRAGS];  // [step's parity]: the two halves' bytes lowest, once shifted down
@@ -205,7 +207,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
     // of a step, the `turn`th of its window
     auto read_scale = [&](int to, uint32_t window, int turn, int i) {
         const int of_step = (turn >> 1) * 128 + (turn & 1) * 8;
-        const uint8_t *at = lds + (window & 1) * Loader::SCALES + (i < TN ? (at_sb ^ of_step) + (i >> 1) * 1024 + (i & 1) * 64 : (at_sa ^ of_step) + (i - TN) * 512);
+        const uint8_t *at = lds + (window & 1) * Loader::SCALES + (i < TN ? (at_sb ^ of_step) + i * 512 : (at_sa ^ of_step) + (i - TN) * 512);
         scale[to][i] = *reinterpret_cast<const uint32_t *>(at);
     };
     // with named accumulators pinned where it stands: no matrix instruction in asm may follow at once that reads it

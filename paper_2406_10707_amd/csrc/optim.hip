@@ -168,7 +168,8 @@ __device__ __forceinline__ f32x4 updated(f32x4 w, f32x4 m, f32x4 v, float keep, 
 // Bound by memory: 32-bit moments move 28 or 30 bytes an element, 8-bit ones 16.1 with gradients in 16 bits. Blocks of one wave in address order keep the chip in a narrow front of each of the seven to
 // nine streams, and shared memory that nothing uses keeps the front narrower still where the grid is larger than the chip: 124 M elements with f32 gradients 609 us, with room for twelve waves to a
 // compute unit 570 = 6.5 TB/s, for seven 596 (two groups a lane: 620, 604, 592; blocks of four waves that loop over a span 665). 8-bit moments need more waves, or more a lane: 405 M
-// elements 1057 us with one group, with two 1084 and, with room for twenty waves, 1055 = 6.2 TB/s (twelve waves: 1760 and 1171); rounding to nearest 1046.
+// elements 1057 us with one group, with two 1084 and, with room for twenty waves, 1055 (twelve waves: 1760 and 1171). Stochastic rounding fills the vector units as well (98 % of their cycles with 80 instructions
+// an element): without the sign of v and with the least code by two integer instructions 1040 us = 6.3 TB/s, rounding to nearest 1050.
 constexpr unsigned kFreeBlocks = 256 * 36;
 constexpr uint32_t kSpansALaunch = 1u << 21;      // a grid has fewer than 2^32 work-items
 // A wave a block, GROUPS groups of four elements a lane, 256 elements apart; kSpan / (256 GROUPS) blocks a span. Every block of 32 elements lies in eight neighbouring lanes.
@@ -226,9 +227,10 @@ __global__ __launch_bounds__(64) void adamw_kernel(const TensorEntry *__restrict
                 uint32_t mc, vc;
                 if constexpr (STOCHASTIC) {
                     const uint64_t r = mix64(a.key + 8 * t.first_block + e / 4);
-                    const uint64_t backwards = (r << 48) | ((r << 16) & 0xFFFF00000000ull) | ((r >> 16) & 0xFFFF0000ull) | (r >> 48);
+                    const uint32_t r_lo = uint32_t(r), r_hi = uint32_t(r >> 32);
+                    const uint64_t backwards = uint64_t(__builtin_amdgcn_alignbit(r_lo, r_lo, 16)) << 32 | __builtin_amdgcn_alignbit(r_hi, r_hi, 16);      // the four fields, last first
                     mc = fp8_stochastic<false>(ym, r);
-                    vc = fp8_stochastic<true>(yv, backwards);
+                    vc = fp8_stochastic<true, false>(yv, backwards);      // squares: never negative
                 } else {
                     mc = fp8_nearest<false>(ym);
                     vc = fp8_nearest<true>(yv);
