@@ -22,12 +22,13 @@ struct TensorEntry {
     double weight_decay;
 };
 
-// What one block works on: `count` elements of a tensor from element `first`, a multiple of 32, on.
+// What one block, or a run of them, works on: `count` elements of a tensor from element `first` on.
 struct Span {
     uint32_t tensor, count;
     uint64_t first;
 };
 constexpr uint32_t kSpan = 4096, kNormBlocks = 1024;
+constexpr uint32_t kGroups32 = 1, kGroups8 = 2;      // groups of 256 elements that a wave of the step takes
 
 struct NormScratch {
     uint64_t partial[kNormBlocks];      // bits of doubles
@@ -39,11 +40,12 @@ struct NormScratch {
 struct ckpt_optim {
     int device = 0;
     size_t n = 0;
-    uint32_t n_spans = 0;
+    uint32_t n_spans = 0;                        // of the norm: tensors cut at every kSpan elements
+    uint32_t n_full = 0, n_pieces = 0;           // of the step: spans of kSpan elements, and what they leave in pieces of a wave each
     ckpt_optim_config cfg{};
     bool has_state = false;
     TensorEntry *dev_tensors = nullptr;
-    Span *dev_spans = nullptr;
+    Span *dev_spans = nullptr, *dev_step_spans = nullptr;
     NormScratch *dev_scratch = nullptr;
     std::vector<uint64_t> numels;
 };
@@ -169,17 +171,18 @@ __device__ __forceinline__ f32x4 updated(f32x4 w, f32x4 m, f32x4 v, float keep, 
 // nine streams, and shared memory that nothing uses keeps the front narrower still where the grid is larger than the chip: 124 M elements with f32 gradients 609 us, with room for twelve waves to a
 // compute unit 570 = 6.5 TB/s, for seven 596 (two groups a lane: 620, 604, 592; blocks of four waves that loop over a span 665). 8-bit moments need more waves, or more a lane: 405 M
 // elements 1057 us with one group, with two 1084 and, with room for twenty waves, 1055 (twelve waves: 1760 and 1171). Stochastic rounding fills the vector units as well (98 % of their cycles with 80 instructions
-// an element): without the sign of v and with the least code by two integer instructions 1040 us = 6.3 TB/s, rounding to nearest 1050.
+// an element): without the sign of v and with the least code by two integer instructions 1040 us, with spans that every block finds work in 1009 = 6.5 TB/s.
 constexpr unsigned kFreeBlocks = 256 * 36;
 constexpr uint32_t kSpansALaunch = 1u << 21;      // a grid has fewer than 2^32 work-items
-// A wave a block, GROUPS groups of four elements a lane, 256 elements apart; kSpan / (256 GROUPS) blocks a span. Every block of 32 elements lies in eight neighbouring lanes.
+// A wave a block, GROUPS groups of four elements a lane, 256 elements apart: kSpan / (256 GROUPS) blocks for each of n_full spans, one for each of the pieces behind them (blocks that find nothing to do
+// cost 1 ns each: 4000 tensors of some 250 elements took 64 us with sixteen for each, 10 so). Every block of 32 elements lies in eight neighbouring lanes.
 // PARAM 0: no working copy. BITS: of the moments.
 template <int GRAD, int PARAM, int BITS, bool STOCHASTIC, int GROUPS>
-__global__ __launch_bounds__(64) void adamw_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ spans, StepArgs a) {
+__global__ __launch_bounds__(64) void adamw_kernel(const TensorEntry *__restrict__ tensors, const Span *__restrict__ full, uint32_t n_full, const Span *__restrict__ pieces, StepArgs a) {
     constexpr uint32_t kWave = 256 * GROUPS, kBlocks = kSpan / kWave;
-    const Span span = spans[blockIdx.x / kBlocks];
-    const uint32_t start = blockIdx.x % kBlocks * kWave;
-    if (start >= span.count) return;
+    const bool piece = blockIdx.x >= n_full * kBlocks;
+    const Span span = *(piece ? pieces + (blockIdx.x - n_full * kBlocks) : full + blockIdx.x / kBlocks);
+    const uint32_t start = piece ? 0 : blockIdx.x % kBlocks * kWave;
     const TensorEntry &t = tensors[span.tensor];
     float scale = 1.0f;
     if (a.norm) {
@@ -260,14 +263,17 @@ __global__ __launch_bounds__(kGradsALaunch) void set_grads_kernel(TensorEntry *t
 template <int GRAD, int PARAM>
 void launch_adamw(const ckpt_optim *o, const StepArgs &a, bool stochastic, hipStream_t stream) {
     auto go = [&](auto kernel, unsigned groups, unsigned lds) {
-        for (uint32_t first = 0; first < o->n_spans; first += kSpansALaunch) {
-            const unsigned blocks = std::min(o->n_spans - first, kSpansALaunch) * (kSpan / 256 / groups);
-            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64), blocks > kFreeBlocks ? lds : 0, stream, o->dev_tensors, o->dev_spans + first, a);
+        for (uint32_t first = 0;; first += kSpansALaunch) {
+            const uint32_t here = std::min(o->n_full - first, kSpansALaunch);
+            const bool last = first + here == o->n_full;
+            const unsigned blocks = here * (kSpan / 256 / groups) + (last ? o->n_pieces : 0);
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64), blocks > kFreeBlocks ? lds : 0, stream, o->dev_tensors, o->dev_step_spans + first, here, o->dev_step_spans + o->n_full, a);
+            if (last) break;
         }
     };
-    if (o->cfg.state_bits == 32) go(adamw_kernel<GRAD, PARAM, 32, false, 1>, 1, 12800);
-    else if (stochastic) go(adamw_kernel<GRAD, PARAM, 8, true, 2>, 2, 8192);
-    else go(adamw_kernel<GRAD, PARAM, 8, false, 2>, 2, 8192);
+    if (o->cfg.state_bits == 32) go(adamw_kernel<GRAD, PARAM, 32, false, kGroups32>, kGroups32, 12800);
+    else if (stochastic) go(adamw_kernel<GRAD, PARAM, 8, true, kGroups8>, kGroups8, 8192);
+    else go(adamw_kernel<GRAD, PARAM, 8, false, kGroups8>, kGroups8, 8192);
 }
 template <int GRAD>
 void launch_adamw(const ckpt_optim *o, const StepArgs &a, bool stochastic, hipStream_t stream) {
@@ -297,7 +303,8 @@ int create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_optim_config *
     o->cfg = *cfg;
     o->n = n;
     std::vector<TensorEntry> entries(n);
-    std::vector<Span> spans;
+    std::vector<Span> spans, full, pieces;
+    const uint32_t wave = 256 * (cfg->state_bits == 32 ? kGroups32 : kGroups8);
     DeviceRanges ranges;
     uint64_t blocks = 0, n_spans = 0;
     bool any = false;
@@ -332,20 +339,39 @@ int create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_optim_config *
         blocks += (t.numel + 31) / 32;
         n_spans += (t.numel + kSpan - 1) / kSpan;
         if (n_spans > 1u << 24) return refuse(CKPT_EINVAL, "more than 2^36 elements");
+        if (state && t.numel) {
+            // 32-bit moments: the spans begin where the master weights begin a line, so that the waves' stores are whole lines (the moments' too, where all lie at the same distance from one, as in
+            // flattened buffers: 85 M elements at any element's address 502 us, so 372). 8-bit ones begin with a block of 32.
+            uint64_t at = 0;
+            const uint64_t head = cfg->state_bits == 32 ? (128 - uint64_t(t.dev_master) % 128) % 128 / 4 : 0;
+            auto piece = [&](uint64_t count) {
+                pieces.push_back(Span{uint32_t(k), uint32_t(count), at});
+                at += count;
+            };
+            if (head && t.numel >= kSpan) piece(head);
+            for (; t.numel - at >= kSpan; at += kSpan) full.push_back(Span{uint32_t(k), kSpan, at});
+            while (at < t.numel) piece(std::min(t.numel - at, uint64_t(wave)));
+        }
+        if (pieces.size() > 1u << 24) return refuse(CKPT_EINVAL, "too many tensors");
         for (uint64_t first = 0; first < t.numel; first += kSpan) spans.push_back(Span{uint32_t(k), uint32_t(t.numel - first < kSpan ? t.numel - first : kSpan), first});
     }
     o->n_spans = uint32_t(spans.size());
+    o->n_full = uint32_t(full.size());
+    o->n_pieces = uint32_t(pieces.size());
+    full.insert(full.end(), pieces.begin(), pieces.end());
     auto failed = [&](hipError_t e) {
-        (void)hipFree(o->dev_tensors); (void)hipFree(o->dev_spans); (void)hipFree(o->dev_scratch);
+        (void)hipFree(o->dev_tensors); (void)hipFree(o->dev_spans); (void)hipFree(o->dev_step_spans); (void)hipFree(o->dev_scratch);
         (void)hipGetLastError();
         return refuse(e == hipErrorOutOfMemory ? CKPT_ENOMEM : CKPT_EHIP, std::string("optimizer set-up: ") + hipGetErrorString(e));
     };
     hipError_t e = hipGetDevice(&o->device);
     if (e == hipSuccess) e = hipMalloc(&o->dev_tensors, n * sizeof(TensorEntry));
     if (e == hipSuccess) e = hipMalloc(&o->dev_spans, (spans.size() + 1) * sizeof(Span));
+    if (e == hipSuccess) e = hipMalloc(&o->dev_step_spans, (full.size() + 1) * sizeof(Span));
     if (e == hipSuccess) e = hipMalloc(&o->dev_scratch, sizeof(NormScratch));
     if (e == hipSuccess) e = hipMemcpy(o->dev_tensors, entries.data(), n * sizeof(TensorEntry), hipMemcpyHostToDevice);
     if (e == hipSuccess && !spans.empty()) e = hipMemcpy(o->dev_spans, spans.data(), spans.size() * sizeof(Span), hipMemcpyHostToDevice);
+    if (e == hipSuccess && !full.empty()) e = hipMemcpy(o->dev_step_spans, full.data(), full.size() * sizeof(Span), hipMemcpyHostToDevice);
     const NormScratch zero{};
     if (e == hipSuccess) e = hipMemcpy(o->dev_scratch, &zero, sizeof zero, hipMemcpyHostToDevice);
     if (e != hipSuccess) return failed(e);
@@ -367,6 +393,7 @@ int ckpt_optim_destroy(ckpt_optim *o) {
         const hipError_t e = hipDeviceSynchronize();
         (void)hipFree(o->dev_tensors);
         (void)hipFree(o->dev_spans);
+        (void)hipFree(o->dev_step_spans);
         (void)hipFree(o->dev_scratch);
         delete o;
         return e == hipSuccess ? CKPT_OK : refuse(CKPT_EHIP, hipGetErrorString(e));
