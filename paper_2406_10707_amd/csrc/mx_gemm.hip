@@ -134,32 +134,11 @@ __device__ __forceinline__ void store_eight(const GemmArgs &p, typename Element<
     }
 }
 
-// Eight consecutive columns of a row of a tile of C: 16 bytes in bf16, twice that in f32.
-template <int OUT> constexpr int kEights = OUT == CKPT_F32 ? 2 : 1;
+// Sixteen bytes of C, with what is there added.
 template <int OUT>
-__device__ __forceinline__ void load_eight_at(u32x4 *old, __amdgpu_buffer_rsrc_t c, uint32_t at, uint32_t uniform) {
-#pragma unroll
-    for (int i = 0; i < kEights<OUT>; i++) old[i] = __builtin_amdgcn_raw_buffer_load_b128(c, at + 16 * i, uniform, 0);
-}
-template <int OUT, bool ADD>
-__device__ __forceinline__ void store_eight_at(__amdgpu_buffer_rsrc_t c, uint32_t at, uint32_t uniform, f32x4 lo, f32x4 hi, const u32x4 *old) {
-    if constexpr (OUT == CKPT_F32) {
-        if constexpr (ADD) {
-            lo += __builtin_bit_cast(f32x4, old[0]);
-            hi += __builtin_bit_cast(f32x4, old[1]);
-        }
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), c, at, uniform, 0);
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), c, at + 16, uniform, 0);
-    } else {
-        typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-        if constexpr (ADD) {
-            const bf16x8 was = __builtin_bit_cast(bf16x8, old[0]);
-            lo += __builtin_convertvector(__builtin_shufflevector(was, was, 0, 1, 2, 3), f32x4);
-            hi += __builtin_convertvector(__builtin_shufflevector(was, was, 4, 5, 6, 7), f32x4);
-        }
-        const bf16x8 both = __builtin_shufflevector(__builtin_convertvector(lo, bf16x4), __builtin_convertvector(hi, bf16x4), 0, 1, 2, 3, 4, 5, 6, 7);
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, both), c, at, uniform, 0);
-    }
+__device__ __forceinline__ u32x4 sum_of_sixteen_bytes(u32x4 sum, u32x4 old) {
+    if constexpr (OUT == CKPT_F32) return __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, sum) + __builtin_bit_cast(f32x4, old));
+    else return sum;
 }
 
 // Four waves, WM x WN, each computing (16 TM) x (16 TN) of the block's tile; ONE wave per SIMD or two. Nothing hides a wait but the wave's own order, so the
@@ -169,7 +148,7 @@ __device__ __forceinline__ void store_eight_at(__amdgpu_buffer_rsrc_t c, uint32_
 // step + 1 have landed for all. (Four steps in LDS: the loads are those of step + 4.) Tiles of more than 32 accumulators a wave name them as AGPRs in the instruction's own operands.
 //
 // 8192^3 takes 237 us = 4640 TFLOP/s with 256 x 256 tiles (gemm_long_kernel 3590): a step 2670 cycles, of which the matrix instructions are 2048, at 1.73 GHz, which the power allows (2.1 GHz
-// without the panels' loads and reads); 7000 cycles in front of a tile's 32 steps and 12,000 behind them, for the stores of C at some 4 TB/s. Scales fetched 16 bytes a row and step cost 14 us
+// without the panels' loads and reads); some 7000 cycles in front of a tile's 32 steps (the first loads of all waves) and 9000 behind them (the stores of C). Scales fetched 16 bytes a row and step cost 14 us
 // more, scales read from LDS at addresses of 2 bytes 150, pieces 2 q + h without the rotation (two lanes a bank) 15.
 template <int WM, int WN, int TM, int TN, int STAGES, int READS, int LOAD_EVERY, int OUT>
 __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrder &order) {
@@ -319,27 +298,70 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
     typedef typename Element<OUT>::one Out;
     const int64_t part = blockIdx.y * p.c_split;
     if (p.vector && row + BM <= p.m && col + BN <= p.n) {
-        // A whole tile: few instructions a store. (With the bounds of each store beside it this was 40 KB of code that every block fetched anew, 190 cycles a store.)
+        // A whole tile goes through LDS, which is free now, so that a store is whole lines of C by neighbouring lanes (straight from the registers neighbouring lanes have different rows): 16384 x 16384 x 4096
+        // 614 -> 573 us, 8192^3 to f32 275 -> 268, 2304 x 768 x 8190 added to f32 17.7 -> 17.1, 1000 x 2304 x 768 to f32 6.6 -> 6.1, 8192^3 to bf16 even, 4096^3 36.2 -> 36.7. A wave has a part of
+        // its own, rows of CP pieces of 16 bytes, of which CH are used; piece p of row r lies at place p ^ f(r). Few instructions a store: with the bounds of each beside it this was 40 KB of
+        // code that every block fetched anew.
+        constexpr int CH = OUT == CKPT_F32 ? 4 * TN : 2 * TN, CP = CH <= 4 ? 4 : CH <= 8 ? 8 : CH <= 16 ? 16 : 32, SHIFT = CP >= 16 ? 0 : CP == 8 ? 1 : 2, MASK = CP >= 16 ? 15 : CP - 1;
+        constexpr int PART = Loader::BYTES / NW, FIT = PART / (16 * 16 * CP), AT_A_TIME = FIT < TM ? FIT : TM, ROWS = 64 / CP;
+        static_assert(FIT >= 1 && PART % 16 == 0, "sixteen rows fit a wave's part");
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // no wave reads its panels any more, and all loads to LDS are over
+        uint8_t *mine = lds + wave * PART;
         Out *tile = static_cast<Out *>(p.c) + part + row * p.ldc + col;
         const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(tile, 0, 0xFFFFFFFFu, 0x00020000);
-        const uint32_t pitch = uint32_t(p.ldc) * sizeof(Out), lane_at = (wm * 16 * TM + ar) * pitch + (wn * 16 * TN + 8 * q) * sizeof(Out);
+        const uint32_t pitch = uint32_t(p.ldc) * sizeof(Out), piece = lane & (CP - 1), lane_row = lane / CP;
+        const uint32_t lane_at = (wm * 16 * TM + lane_row) * pitch + wn * 16 * TN * sizeof(Out) + 16 * piece;
         auto store_tile = [&](auto add) {
-            constexpr int PAIRS = TN / 2, E = kEights<OUT>;
-            u32x4 old[2][PAIRS * E];      // what is there, a row of fragments ahead
-            auto load_row = [&](int i) {
 #pragma unroll
-                for (int j = 0; j < PAIRS; j++) load_eight_at<OUT>(&old[i & 1][j * E], rc, lane_at + 32 * j * sizeof(Out), 16 * i * pitch);
-            };
-            if constexpr (add) load_row(0);
+            for (int i0 = 0; i0 < TM; i0 += AT_A_TIME) {
 #pragma unroll
-            for (int i = 0; i < TM; i++) {
-                if constexpr (add)
-                    if (i + 1 < TM) load_row(i + 1);
+                for (int i = i0; i < i0 + AT_A_TIME && i < TM; i++)
 #pragma unroll
-                for (int j = 0; j < PAIRS; j++) {
-                    // in their registers up to here: copied out all at once they would spill
-                    if constexpr (NAMED) asm volatile("" : "+a"(acc[i][2 * j]), "+a"(acc[i][2 * j + 1]));
-                    store_eight_at<OUT, add>(rc, lane_at + 32 * j * sizeof(Out), 16 * i * pitch, acc[i][2 * j], acc[i][2 * j + 1], &old[i & 1][j * E]);
+                    for (int j = 0; j < TN; j += 2) {
+                        // in their registers up to here: copied out all at once they would spill
+                        if constexpr (NAMED) asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
+                        uint8_t *at = mine + (16 * (i - i0) + ar) * (16 * CP);
+                        const int f = (ar >> SHIFT) & MASK;
+                        if constexpr (OUT == CKPT_F32) {
+                            *reinterpret_cast<f32x4 *>(at + 16 * ((4 * j + 2 * q) ^ f)) = acc[i][j];
+                            *reinterpret_cast<f32x4 *>(at + 16 * ((4 * j + 2 * q + 1) ^ f)) = acc[i][j + 1];
+                        } else {
+                            f32x4 lo = acc[i][j], hi = acc[i][j + 1];
+                            if constexpr (add) {      // before the rounding
+                                const uint32_t there = (wm * 16 * TM + ar) * pitch + (wn * 16 * TN + 16 * j + 8 * q) * sizeof(Out);
+                                typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+                                const bf16x8 old = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rc, there, 16 * i * pitch, 0));
+                                lo += __builtin_convertvector(__builtin_shufflevector(old, old, 0, 1, 2, 3), f32x4);
+                                hi += __builtin_convertvector(__builtin_shufflevector(old, old, 4, 5, 6, 7), f32x4);
+                            }
+                            typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+                            *reinterpret_cast<bf16x8 *>(at + 16 * ((2 * j + q) ^ f)) =
+                                __builtin_shufflevector(__builtin_convertvector(lo, bf16x4), __builtin_convertvector(hi, bf16x4), 0, 1, 2, 3, 4, 5, 6, 7);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                constexpr int COUNT = 16 * AT_A_TIME / ROWS, BATCH = 8;
+                const int left = (TM - i0 < AT_A_TIME ? 16 * (TM - i0) : 16 * AT_A_TIME) / ROWS;
+#pragma unroll
+                for (int t0 = 0; t0 < COUNT; t0 += BATCH) {
+                    if (t0 >= left) break;
+                    u32x4 old[BATCH], sum[BATCH];
+                    if (CH < CP && piece >= CH) continue;
+                    if constexpr (add && OUT == CKPT_F32)
+#pragma unroll
+                        for (int t = 0; t < BATCH; t++)
+                            if (t0 + t < left) old[t] = __builtin_amdgcn_raw_buffer_load_b128(rc, lane_at, (16 * i0 + ROWS * (t0 + t)) * pitch, 0);
+#pragma unroll
+                    for (int t = 0; t < BATCH; t++) {
+                        const int r = ROWS * (t0 + t) + lane_row;
+                        if (t0 + t < left) sum[t] = *reinterpret_cast<const u32x4 *>(mine + r * (16 * CP) + 16 * (piece ^ ((r >> SHIFT) & MASK)));
+                    }
+#pragma unroll
+                    for (int t = 0; t < BATCH; t++)
+                        if (t0 + t < left) {
+                            if constexpr (add && OUT == CKPT_F32) sum[t] = sum_of_sixteen_bytes<OUT>(sum[t], old[t]);
+                            __builtin_amdgcn_raw_buffer_store_b128(sum[t], rc, lane_at, (16 * i0 + ROWS * (t0 + t)) * pitch, 0);
+                        }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }

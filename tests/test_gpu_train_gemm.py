@@ -77,6 +77,24 @@ def test_products_are_exact(out, accumulate):
         assert np.array_equal(got, exactly(want + before if accumulate else want, out))
 
 
+# a shape of whole tiles and one of ragged ones for every form (the names are those of the table in csrc/mx_gemm_forms.hpp; tests/test_host_train_forms.py asks it)
+FORMS = {"256x256": [(3328, 3328, 1024), (3300, 3400, 1000)], "192x192": [(2496, 3264, 2048), (2500, 3300, 2000)], "128x128": [(2048, 2048, 2048), (2000, 2050, 1030)],
+         "64x128": [(2048, 2048, 1024), (2040, 1950, 1000)], "64x64 four stages": [(1024, 1024, 1024), (500, 1030, 2000)], "64x64 two stages": [(1024, 2304, 768), (1000, 2300, 700)]}
+
+
+@pytest.mark.parametrize("out,accumulate", [("bf16", False), ("f32", True), ("bf16", True), ("f32", False)])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_every_form(form, out, accumulate):
+    for m, n, k in FORMS[form]:
+        print(f"form {form}: {m} x {n} x {k} {out} accumulate {accumulate}", flush=True)
+        rng = np.random.default_rng(m + n)
+        a, b = operand(m, k, rng, 0), operand(n, k, rng, 0)
+        want, magnitude = to.gemm(to.values(*a, to.MXFP4).astype(np.float32), to.values(*b, to.MXFP4).astype(np.float32))      # exact in f32 as well
+        assert magnitude.max() + 64 < 2.0 ** 22
+        got, before = product(a, b, m, n, k, out, accumulate, 0, rng, workspace=False)
+        assert np.array_equal(got, exactly(want.astype(np.float64) + before if accumulate else want, out))
+
+
 @pytest.mark.parametrize("out,accumulate", [("bf16", True), ("f32", False)])
 @pytest.mark.parametrize("m,n,k", [(17, 64, 16384), (64, 512, 16384), (25, 70, 17000), (130, 100, 20000), (30, 1001, 16000)])
 def test_parts_of_a_long_axis(m, n, k, out, accumulate):

@@ -5,6 +5,8 @@ import subprocess
 
 import pytest
 
+from tests.test_gpu_train_gemm import FORMS
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MAIN = """#include <cstdio>
 #include "mx_gemm_forms.hpp"
@@ -36,6 +38,12 @@ def ask(tmp_path_factory):
 def test_every_form_is_some_sizes(ask):
     sizes = [(8192, 8192, 8192, 0), (2048, 4096, 11008, 0), (2048, 2048, 2048, 0), (2304, 768, 8190, 1), (40, 11008, 4096, 0), (1000, 2304, 768, 0)]
     assert [name for name, _, _ in ask(sizes)] == ["256x256", "192x192", "128x128", "64x128", "64x64 four stages", "64x64 two stages"]
+
+
+def test_the_forms_that_the_gpu_tests_stand_for(ask):
+    for name, shapes in FORMS.items():
+        for shape in shapes:
+            assert [x[0] for x in ask([(*shape, 0, 0), (*shape, 1, 0)])] == [name] * 2, (name, shape)
 
 
 def test_grids_count_in_32_bits(ask):
