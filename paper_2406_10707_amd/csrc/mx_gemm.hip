@@ -340,6 +340,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
+                asm volatile("" ::: "memory");      // other lanes' writes are read: a wave's go to LDS in the order of the program, which the compiler must not change
                 constexpr int COUNT = 16 * AT_A_TIME / ROWS, BATCH = 8;
                 const int left = (TM - i0 < AT_A_TIME ? 16 * (TM - i0) : 16 * AT_A_TIME) / ROWS;
 #pragma unroll
@@ -364,6 +365,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
                         }
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                asm volatile("" ::: "memory");
             }
         };
         if (p.accumulate) store_tile(std::true_type{});
