@@ -116,11 +116,11 @@ typedef struct {
 } ckpt_norm_result;
 
 /* grad_scale: what gradients are to be multiplied with in any case (1 / (loss scale * accumulated batches)).
- * max_norm <= 0: no clipping. Sums in 64 bits. With a nonfinite gradient scale is 0. */
+ * At least 0. max_norm <= 0: no clipping. Sums in 64 bits. With a nonfinite gradient scale is 0. */
 int ckpt_optim_grad_norm(ckpt_optim *opt, double max_norm, double grad_scale, ckpt_norm_result *dev_out, void *stream);
 
 typedef struct {
-    double lr, beta1, beta2, eps;      /* eps at least 1e-30 */
+    double lr, beta1, beta2, eps;      /* eps at least 1e-30; below 1e-12 v may reach 2e31 (1 - beta2^step), else 3e38 of it */
     uint64_t step;                     /* 1, 2, ... */
     uint64_t seed;                     /* stochastic rounding */
     int32_t rounding;                  /* of 8-bit moments: CKPT_ROUND_NEAREST or CKPT_ROUND_STOCHASTIC */

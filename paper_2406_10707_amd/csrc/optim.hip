@@ -145,7 +145,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const TensorEntry *__rest
 // ------------------------------------------------------------------ AdamW step
 
 struct StepArgs {
-    float beta1, one_less_beta1, beta2, one_less_beta2, eps, lr, inv_bc1, inv_bc2;
+    float beta1, one_less_beta1, beta2, one_less_beta2, eps, lr, inv_bc1, inv_bc2, root_back;
     double lr64;
     uint64_t key;
     const ckpt_norm_result *norm;
@@ -157,11 +157,13 @@ __device__ __forceinline__ void update_moments(f32x4 g, f32x4 &m, f32x4 &v, cons
     m = m * a.beta1 + g * a.one_less_beta1;
     v = v * a.beta2 + (g * g) * a.one_less_beta2;
 }
-// The root and the quotient by the approximate instructions (1 ulp each): the error is 1e-7 of the update, which is some 1e-4 of the weight.
+// The root and the quotient by the approximate instructions (1 ulp each): the error is 1e-7 of the update, which is some 1e-4 of the weight. The root's takes subnormal numbers as zero, which is up to 1.1e-19
+// of the root: beside a smaller eps than kSmallEps inv_bc2 comes multiplied by 2^24, and root_back divides by 2^12 (else 1; in the addition's own instruction either way).
+constexpr double kSmallEps = 1e-12;
 __device__ __forceinline__ f32x4 updated(f32x4 w, f32x4 m, f32x4 v, float keep, const StepArgs &a) {
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        const float root = __builtin_amdgcn_sqrtf(v[j] * a.inv_bc2) + a.eps;
+        const float root = __builtin_fmaf(__builtin_amdgcn_sqrtf(v[j] * a.inv_bc2), a.root_back, a.eps);
         w[j] = w[j] * keep - a.lr * (m[j] * a.inv_bc1 * __builtin_amdgcn_rcpf(root));
     }
     return w;
@@ -425,7 +427,7 @@ int ckpt_optim_set_grads(ckpt_optim *o, const void *const *dev_grads, size_t n, 
 int ckpt_optim_grad_norm(ckpt_optim *o, double max_norm, double grad_scale, ckpt_norm_result *dev_out, void *hip_stream) {
     return at_c_entry([&] {
         if (!o) return refuse(CKPT_EINVAL, "null argument");
-        if (!(max_norm == max_norm) || !(fabs(grad_scale) <= 1e30)) return refuse(CKPT_EINVAL, "max_norm or grad_scale is not a number");
+        if (!(max_norm == max_norm) || !(grad_scale >= 0 && grad_scale <= 1e30)) return refuse(CKPT_EINVAL, "max_norm is not a number, or grad_scale negative or not one");
         if (int r = wrong_device(o)) return r;
         DeviceRanges ranges;
         if (const char *why = ranges.wrong(dev_out, sizeof *dev_out)) return refuse(CKPT_EINVAL, std::string("dev_out: ") + why);
@@ -467,7 +469,8 @@ int ckpt_optim_adamw_step(ckpt_optim *o, const ckpt_adamw_args *p, void *hip_str
         a.lr = float(p->lr);
         a.lr64 = p->lr;
         a.inv_bc1 = float(1.0 / (1.0 - pow(p->beta1, double(p->step))));
-        a.inv_bc2 = float(1.0 / (1.0 - pow(p->beta2, double(p->step))));
+        a.inv_bc2 = float((p->eps < kSmallEps ? 0x1p24 : 1.0) / (1.0 - pow(p->beta2, double(p->step))));
+        a.root_back = p->eps < kSmallEps ? 0x1p-12f : 1.0f;
         a.key = mix64(mix64(p->seed) + p->step);
         a.norm = p->dev_norm;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

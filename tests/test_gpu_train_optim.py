@@ -276,6 +276,37 @@ def test_the_moments_follow_differences_of_the_loss():
     assert loss(got) < loss(w64)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-8, 1e-12, 0.99e-12, 1e-15, 1e-20, 1e-25])
+def test_second_moments_below_the_normal_numbers(bits, eps):
+    """The root of a subnormal number counts where eps is as small; both sides of the rule that chooses how it is taken. The bound: as in check()."""
+    print(f"adamw, subnormal second moments, eps {eps}, {bits} bits", flush=True)
+    rng = np.random.default_rng(5)
+    n = 4096 + 700
+    v = (10.0 ** rng.uniform(-44, -36, n)).astype(np.float32)
+    m = (rng.standard_normal(n) * np.sqrt(v.astype(np.float64))).astype(np.float32)
+    w, g = np.zeros(n, np.float32), np.zeros(n, np.float32)
+    arena = Arena(n * 20 + 16384)
+    t = dict(numel=n, weight_decay=0.0, grad=arena.add(g, 4, 0), master=arena.add(w, 4, 0))
+    if bits == 32:
+        t |= dict(m=arena.add(m, 4, 0), v=arena.add(v, 4, 0))
+    else:
+        for name, x in (("m", m), ("v", v)):
+            c, b = to.moment8(x, nonzero=name == "v")
+            t |= {name: arena.add(c, 1, 0), name + "_scale": arena.add(b, 1, 0)}
+            x[:] = to.values(c.reshape(1, -1), b.reshape(1, -1), to.MXFP8).reshape(-1)
+    arena.upload()
+    opt = B.Optimizer([t], grad_dtype=B.CKPT_F32, param_dtype=0, state_bits=bits)
+    hyper = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=eps, step=7)
+    opt.step(0, **hyper)
+    harness.synchronize()
+    arena.fetch()
+    m, v = to.moments(m, v, g, 1.0, 0.9, 0.95)
+    assert np.count_nonzero((v > 0) & (v < 2.0 ** -126)) > 500
+    want, update = to.adamw(w, m, v, weight_decay=0.0, **hyper)
+    assert np.all(np.abs(arena.read(1).view(np.float32) - want) <= 2.0 ** -19 * np.abs(update) + 1e-38)
+
+
 def test_a_nonfinite_gradient_without_the_norm_spoils_its_block_alone():
     print("infinity in a block", flush=True)
     s = Setup([1000], "f32", "bf16", 8, seed=12)
@@ -366,3 +397,13 @@ def test_what_is_refused():
             opt.grad_norm(stream=0, **bad)
         assert e.value.code == B.CKPT_EINVAL
     harness.synchronize()
+
+
+def test_a_negative_grad_scale_is_refused():
+    """It would make the norm negative, and nothing would be clipped."""
+    print("negative grad_scale", flush=True)
+    buf = harness.DevBuf(4096)
+    opt = B.Optimizer([dict(numel=64, grad=buf.ptr)], grad_dtype=B.CKPT_F32)
+    with pytest.raises(B.CkptError) as e:
+        opt.grad_norm(buf.ptr + 1024, 0, max_norm=1.0, grad_scale=-1.0)
+    assert e.value.code == B.CKPT_EINVAL
