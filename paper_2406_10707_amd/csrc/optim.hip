@@ -30,9 +30,10 @@ struct Span {
 constexpr uint32_t kSpan = 4096, kNormBlocks = 1024;
 constexpr uint32_t kGroups32 = 1, kGroups8 = 2;      // groups of 256 elements that a wave of the step takes
 
+constexpr uint32_t kNormGroups = 32, kUngrouped = 64;      // blocks are counted in groups, each on a line of its own, where there are more than kUngrouped
 struct NormScratch {
     uint64_t partial[kNormBlocks];      // bits of doubles
-    uint32_t arrived;
+    struct { uint32_t arrived, unused[31]; } group[kNormGroups], all;
 };
 
 }  // namespace
@@ -121,10 +122,18 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const TensorEntry *__rest
         // value, not from a release (which writes the whole L2 back: 36 ns a block, one behind the other).
         const uint64_t before = __hip_atomic_exchange(&scratch->partial[blockIdx.x], uint64_t(__double_as_longlong(sum_of_parts(part))), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::"v"(before) : "memory");
-        last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        uint32_t wanted = gridDim.x;
+        bool counts = true;      // the last of a group stands for all of it
+        if (gridDim.x > kUngrouped) {
+            const uint32_t g = blockIdx.x % kNormGroups, members = (gridDim.x - g + kNormGroups - 1) / kNormGroups;
+            counts = __hip_atomic_fetch_add(&scratch->group[g].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == members - 1;
+            wanted = kNormGroups;
+        }
+        last = counts && __hip_atomic_fetch_add(&scratch->all.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == wanted - 1;
     }
     __syncthreads();
     if (!last) return;
+    if (threadIdx.x < kNormGroups) __hip_atomic_store(&scratch->group[threadIdx.x].arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sum = 0;
     for (uint32_t b = threadIdx.x; b < gridDim.x; b += THREADS) sum += __longlong_as_double(int64_t(__hip_atomic_load(&scratch->partial[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
     sum = sum_over_wave(sum);
@@ -132,7 +141,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const TensorEntry *__rest
     __syncthreads();
     if (threadIdx.x) return;
     sum = sum_of_parts(part);
-    __hip_atomic_store(&scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&scratch->all.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool finite = sum < __longlong_as_double(0x7FF0000000000000ll);
     const double norm = grad_scale * sqrt(sum);
     out->sum_squares = sum;
