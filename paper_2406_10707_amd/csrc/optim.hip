@@ -62,10 +62,11 @@ __device__ __forceinline__ double sum_over_wave(double v) {
 }
 
 // One pass over all gradients, squares in 64 bits (no f32 gradient overflows them, and only an infinity or a NaN makes the sum one); a block's sum goes to its place in the scratch memory, the
-// block that finds itself the last adds them up in order. Bound by memory: 124 M f32 gradients 72 us = 6.9 TB/s, 405 M bf16 121 us = 6.7 TB/s. Some 8 MB have to be under way: f32 with 512 blocks of 256
-// (1024: 76 us, 256: 110), two bytes with 1024 of 512 (512: 160). Counting itself is some 10 ns a block, so short lists have a block for every sixteen spans (4.5 M bf16: 256 blocks 10 us, 1024 16).
+// block that finds itself the last adds them up in order. Bound by memory: 124 M f32 gradients 70 to 72 us = 6.9 TB/s, 405 M bf16 119 us = 6.8 TB/s. Some 8 MB have to be under way: f32 with 512 blocks of 256
+// (1024: 73 us, 512 of 512: 82), two bytes with 1024 of 512 (512: 160). One counter takes some 10 ns a block, one behind the other; with a counter for each of 32 groups 56 M bf16 take 20 us (one counter: 26),
+// 1 M 4.4 (6.1), and blocks pay from four spans each on (16 M bf16 8.4 us, with one for every sixteen 13.3).
 inline uint32_t norm_blocks(uint32_t n_spans, uint32_t most) {
-    const uint32_t wanted = n_spans / 16 < 256 ? 256 : n_spans / 16 > most ? most : n_spans / 16;
+    const uint32_t wanted = n_spans / 4 < 256 ? 256 : n_spans / 4 > most ? most : n_spans / 4;
     return n_spans < 1 ? 1 : n_spans < wanted ? n_spans : wanted;
 }
 
