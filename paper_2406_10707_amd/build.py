@@ -9,7 +9,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdsllm_ckpt.so")
 SOURCES = ["plan.cpp", "engine.cpp", "submit.cpp", "io_threads.cpp", "restore.cpp", "second_tier.cpp", "pack_kernels.hip",
            "pack_image.hip", "derive_kernels.hip", "proxy_kernels.hip", "optim.hip", "mx_quantize.hip", "mx_gemm.hip"]
-HEADERS = ["plan.hpp", "engine_internal.hpp", "tile_batch.hpp", "kernel_util.hpp", "gemm_forms.hpp", "gemm_tile.hpp", "mx_gemm_forms.hpp", "train_util.hpp",
+HEADERS = ["plan.hpp", "engine_internal.hpp", "tile_batch.hpp", "kernel_util.hpp", "gemm_forms.hpp", "gemm_tile.hpp", "mx_gemm_forms.hpp", "mx_gemm_loader.hpp", "train_util.hpp",
            *(os.path.join("..", "..", "include", h) for h in ("ckpt.h", "ckpt_proxy.h", "ckpt_train.h"))]
 
 HIPCC_FLAGS = [
