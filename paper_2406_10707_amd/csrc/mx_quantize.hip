@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
 #pragma unroll
         for (int k = 0; k < int(kGroups); k++) {
             const uint64_t col = first + 512 * k + 8 * lane, random = a.key + row * ((a.cols + 3) / 4) + col / 4;
-            f32x4 lo = __builtin_convertvector(x[k].lo, f32x4), hi = __builtin_convertvector(x[k].hi, f32x4);
+            const f32x4 lo = __builtin_convertvector(x[k].lo, f32x4), hi = __builtin_convertvector(x[k].hi, f32x4);
             uint32_t byte;
             if constexpr (FORMAT == CKPT_MXFP4) {
                 uint32_t codes = fp4_codes_of_eight<STOCHASTIC>(lo, hi, random, &byte);
@@ -65,10 +65,9 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
                 if (col / 2 < a.code_pitch) *(uint32_t DSLLM_GLOBAL *)(a.codes + row * a.code_pitch + col / 2) = codes;
             } else {
                 byte = scale_byte<CKPT_MXFP8>(most_of_4(max(magnitude_bits(lo), magnitude_bits(hi))));
-                lo *= inverse_scale(byte);
-                hi *= inverse_scale(byte);
-                const uint32_t c0 = STOCHASTIC ? fp8_stochastic<NONZERO>(lo, mix64(random)) : fp8_nearest<NONZERO>(lo);
-                const uint32_t c1 = STOCHASTIC ? fp8_stochastic<NONZERO>(hi, mix64(random + 1)) : fp8_nearest<NONZERO>(hi);
+                const f32x4 y0 = lo * inverse_scale(byte), y1 = hi * inverse_scale(byte);
+                const uint32_t c0 = STOCHASTIC ? fp8_stochastic<NONZERO>(y0, lo, mix64(random)) : fp8_nearest<NONZERO>(y0, lo);
+                const uint32_t c1 = STOCHASTIC ? fp8_stochastic<NONZERO>(y1, hi, mix64(random + 1)) : fp8_nearest<NONZERO>(y1, hi);
                 uint8_t *at = a.codes + row * a.code_pitch + col;
                 if (whole || count[k] == 8) {
                     typedef u32x2 two_bytealigned __attribute__((aligned(1)));

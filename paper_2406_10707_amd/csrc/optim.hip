@@ -244,11 +244,11 @@ __global__ __launch_bounds__(64) void adamw_kernel(const TensorEntry *__restrict
                     const uint64_t r = mix64(a.key + 8 * t.first_block + e / 4);
                     const uint32_t r_lo = uint32_t(r), r_hi = uint32_t(r >> 32);
                     const uint64_t backwards = uint64_t(__builtin_amdgcn_alignbit(r_lo, r_lo, 16)) << 32 | __builtin_amdgcn_alignbit(r_hi, r_hi, 16);      // the four fields, last first
-                    mc = fp8_stochastic<false>(ym, r);
-                    vc = fp8_stochastic<true, false>(yv, backwards);      // squares: never negative
+                    mc = fp8_stochastic<false>(ym, m[k], r);
+                    vc = fp8_stochastic<true, false>(yv, v[k], backwards);      // squares: never negative
                 } else {
-                    mc = fp8_nearest<false>(ym);
-                    vc = fp8_nearest<true>(yv);
+                    mc = fp8_nearest<false>(ym, m[k]);
+                    vc = fp8_nearest<true>(yv, v[k]);
                 }
                 store_bytes(t.m + e, mc, count[k]);
                 store_bytes(t.v + e, vc, count[k]);

@@ -205,22 +205,23 @@ __device__ __forceinline__ uint32_t fp4_stochastic(f32x4 y, uint64_t random) {
     }
     return r;
 }
-// E4M3 codes of four values of at most 448, element 0 in the lowest byte. NaN gives some code (its block's scale says NaN). NONZERO: what is not zero is at least code 1.
+// E4M3 codes of four values y = x / scale of at most 448, element 0 in the lowest byte. NaN gives some code (its block's scale says NaN). NONZERO: what is not zero is at least code 1. That
+// is x's to say: y is zero where x lies 2^149 and more below the block's largest.
 template <bool NONZERO>
-__device__ __forceinline__ uint32_t fp8_nearest(f32x4 y) {
+__device__ __forceinline__ uint32_t fp8_nearest(f32x4 y, f32x4 x) {
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     r = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
     uint32_t codes = uint32_t(r);
     if (NONZERO) {
 #pragma unroll
         for (int j = 0; j < 4; j++)
-            if (y[j] != 0 && !(codes & (0x7Fu << (8 * j)))) codes |= 1u << (8 * j);
+            if (x[j] != 0 && !(codes & (0x7Fu << (8 * j)))) codes |= 1u << (8 * j);
     }
     return codes;
 }
 // From 2^-6 on a code is the upper bits of the f32 pattern, the twenty below are rounded away; smaller values are multiples of 2^-9. SIGNED: there may be negative ones.
 template <bool NONZERO, bool SIGNED = true>
-__device__ __forceinline__ uint32_t fp8_stochastic(f32x4 y, uint64_t random) {
+__device__ __forceinline__ uint32_t fp8_stochastic(f32x4 y, f32x4 x, uint64_t random) {
     uint32_t r = 0;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
@@ -229,7 +230,7 @@ __device__ __forceinline__ uint32_t fp8_stochastic(f32x4 y, uint64_t random) {
         const uint32_t normal = ((__float_as_uint(a) + (bits << 4)) >> 20) - 960u;
         const uint32_t small = (uint32_t(fminf(a, 0.015625f) * 33554432.0f) + bits) >> 16;
         uint32_t code = a >= 0.015625f ? normal : small;
-        if (NONZERO) code = max(code, min(__float_as_uint(a), 1u));
+        if (NONZERO) code = max(code, min(__float_as_uint(SIGNED ? fabsf(x[j]) : x[j]), 1u));
         if (SIGNED) code = (code & 0x7Fu) | (__float_as_uint(y[j]) >> 31 << 7);
         else code &= 0xFFu;
         r |= code << (8 * j);
