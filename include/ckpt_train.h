@@ -111,12 +111,13 @@ typedef struct {
     double sum_squares;      /* of all gradients as they are, for a sum over ranks */
     float norm;              /* grad_scale * sqrt(sum_squares) */
     float scale;             /* what the step multiplies gradients with: grad_scale * min(1, max_norm / norm) */
-    int32_t nonfinite;       /* 1: a gradient is an infinity or a NaN; the step then changes nothing */
+    int32_t nonfinite;       /* 1: a gradient is an infinity or a NaN, or f32 does not hold what the step would make of them: norm
+                                above f32's largest, or what clipping leaves of it above 2^63. The step then changes nothing */
     int32_t reserved;
 } ckpt_norm_result;
 
 /* grad_scale: what gradients are to be multiplied with in any case (1 / (loss scale * accumulated batches)).
- * At least 0. max_norm <= 0: no clipping. Sums in 64 bits. With a nonfinite gradient scale is 0. */
+ * At least 0. max_norm <= 0: no clipping. Sums in 64 bits. With nonfinite set scale is 0. */
 int ckpt_optim_grad_norm(ckpt_optim *opt, double max_norm, double grad_scale, ckpt_norm_result *dev_out, void *stream);
 
 typedef struct {
@@ -136,7 +137,7 @@ typedef struct {
  * that is not zero is never rounded to zero (the next step divides by its root). With beta2 near 1 a step changes v by less than half a
  * code, which rounding to nearest undoes for ever: long runs round stochastically. Element i of a tensor takes field i mod 4 of
  * mix(mix(mix(seed) + step) + 8 * (blocks of all tensors before) + i / 4) for m, field 3 - i mod 4 for v. A block with an
- * infinite or NaN moment becomes NaN as a whole: give dev_norm, and such a step is left out. */
+ * infinite or NaN moment becomes NaN as a whole: give dev_norm, and a step that would make one is left out. */
 int ckpt_optim_adamw_step(ckpt_optim *opt, const ckpt_adamw_args *args, void *stream);
 
 #ifdef __cplusplus

@@ -143,12 +143,14 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const TensorEntry *__rest
     if (threadIdx.x) return;
     sum = sum_of_parts(part);
     __hip_atomic_store(&scratch->all.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool finite = sum < __longlong_as_double(0x7FF0000000000000ll);
+    // An infinity or a NaN makes the sum one (and fails every comparison). A step squares scale * gradient in f32, which holds 2^64 squared no more; up to 2^63 a second moment has room for
+    // being rounded up in 8 bits.
     const double norm = grad_scale * sqrt(sum);
+    const bool clipped = max_norm > 0 && norm > max_norm, usable = norm <= double(__FLT_MAX__) && (clipped ? max_norm : norm) <= 0x1p63;
     out->sum_squares = sum;
     out->norm = float(norm);
-    out->scale = !finite ? 0.0f : max_norm > 0 && norm > max_norm ? float(grad_scale * (max_norm / norm)) : float(grad_scale);
-    out->nonfinite = finite ? 0 : 1;
+    out->scale = !usable ? 0.0f : clipped ? float(grad_scale * (max_norm / norm)) : float(grad_scale);
+    out->nonfinite = usable ? 0 : 1;
     out->reserved = 0;
 }
 
