@@ -101,7 +101,7 @@ typedef struct {
  * Tensors must not overlap. A handle belongs to the device that was current, and to one stream at a time (its
  * ckpt_optim_grad_norm calls share scratch memory). */
 int ckpt_optim_create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_optim_config *cfg, ckpt_optim **out);
-/* Waits for the device, then frees the handle. */
+/* Waits for the handle's device, whichever is current, then frees the handle. */
 int ckpt_optim_destroy(ckpt_optim *opt);
 /* New gradient addresses, one for each tensor, for work enqueued behind this on the stream. */
 int ckpt_optim_set_grads(ckpt_optim *opt, const void *const *dev_grads, size_t n, void *stream);

@@ -404,11 +404,15 @@ int ckpt_optim_create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_opt
 int ckpt_optim_destroy(ckpt_optim *o) {
     return at_c_entry([&] {
         if (!o) return refuse(CKPT_EINVAL, "null argument");
-        const hipError_t e = hipDeviceSynchronize();
+        int current = o->device;      // the caller's may be another device than the one whose work is to be waited for
+        (void)hipGetDevice(&current);
+        hipError_t e = current == o->device ? hipSuccess : hipSetDevice(o->device);
+        if (e == hipSuccess) e = hipDeviceSynchronize();
         (void)hipFree(o->dev_tensors);
         (void)hipFree(o->dev_spans);
         (void)hipFree(o->dev_step_spans);
         (void)hipFree(o->dev_scratch);
+        if (current != o->device) (void)hipSetDevice(current);
         delete o;
         return e == hipSuccess ? CKPT_OK : refuse(CKPT_EHIP, hipGetErrorString(e));
     });
