@@ -438,11 +438,37 @@ __global__ __launch_bounds__(256) void gemm_long_kernel(GemmArgs p) {
             }
 }
 
+// The product in parts of at most `rows` x `columns` of C, a launch each: one grid has fewer than 2^32 work-items along each axis, and 65535 blocks down.
+template <int OUT, class F>
+void launch_in_parts(const GemmArgs &p, int64_t rows, int64_t columns, F launch) {
+    for (int64_t row = 0; row < p.m; row += rows)
+        for (int64_t col = 0; col < p.n; col += columns) {
+            GemmArgs part = p;
+            part.a += row * p.a_pitch;
+            part.b += col * p.b_pitch;
+            part.a_scale += row * p.a_scale_pitch;
+            part.b_scale += col * p.b_scale_pitch;
+            part.c = static_cast<typename Element<OUT>::one *>(p.c) + row * p.ldc + col;
+            part.m = std::min(rows, p.m - row);
+            part.n = std::min(columns, p.n - col);
+            launch(part);
+        }
+}
+
 template <int OUT>
 void launch_few(uint32_t waves, const GemmArgs &p, hipStream_t stream) {
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((p.n + 15) / 16)), dim3(64 * waves), 0, stream, p); };
-    if (waves == 2) go(gemm_few_kernel<2, OUT>);
-    else go(gemm_few_kernel<4, OUT>);
+    launch_in_parts<OUT>(p, 16, 16ll << 23, [&](const GemmArgs &part) {
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((part.n + 15) / 16)), dim3(64 * waves), 0, stream, part); };
+        if (waves == 2) go(gemm_few_kernel<2, OUT>);
+        else go(gemm_few_kernel<4, OUT>);
+    });
+}
+
+template <int OUT>
+void launch_long(const GemmArgs &p, hipStream_t stream) {
+    launch_in_parts<OUT>(p, 64ll << 15, 64ll << 23, [&](const GemmArgs &part) {
+        hipLaunchKernelGGL(gemm_long_kernel<OUT>, dim3(unsigned((part.n + 63) / 64), unsigned((part.m + 63) / 64)), dim3(256), 0, stream, part);
+    });
 }
 
 // The parts' sums of a product whose K was split, added in order. Rows of the parts are `pitch` elements apart, a multiple of 4.
@@ -528,10 +554,8 @@ int gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t dtyp
         else launch_form<CKPT_BF16>(choice.form, 1, p, stream);
         return launched();
     }
-    const dim3 grid(unsigned((n + 63) / 64), unsigned((m + 63) / 64));
-    if (grid.y > 65535) return refuse(CKPT_EINVAL, "too many rows");
-    if (dtype == CKPT_F32) hipLaunchKernelGGL(gemm_long_kernel<CKPT_F32>, grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL(gemm_long_kernel<CKPT_BF16>, grid, dim3(256), 0, stream, p);
+    if (dtype == CKPT_F32) launch_long<CKPT_F32>(p, stream);
+    else launch_long<CKPT_BF16>(p, stream);
     return launched();
 }
 

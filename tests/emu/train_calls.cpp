@@ -1,7 +1,6 @@
 // The host side of the training operators on a HIP runtime of this file's own: two devices, allocations by decree (nothing is behind their addresses), a record of every call and launch.
 // The sources are compiled for the host alone, so a launch comes here with its grid and its arguments.
-#include <hip/hip_runtime_api.h>
-
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -10,6 +9,7 @@
 
 #include "../../include/ckpt.h"
 #include "../../include/ckpt_train.h"
+#include "../../paper_2406_10707_amd/csrc/mx_gemm_loader.hpp"
 
 namespace dsllm { thread_local std::string g_last_error; }
 
@@ -29,7 +29,6 @@ static const Allocation *allocation_of(const void *p) {
 }
 
 extern "C" {
-char __hip_fatbin[1], __hip_fatbin_optim[1];
 void **__hipRegisterFatBinary(const void *) { static void *h; return &h; }
 void __hipUnregisterFatBinary(void **) {}
 static std::vector<std::pair<const void *, std::string>> &kernels() { static std::vector<std::pair<const void *, std::string>> k; return k; }
@@ -97,9 +96,52 @@ static void destroy_on_another_device() {
     for (size_t i = 1; i < calls.size(); i++) REQUIRE(calls[i] == "free on 1");
 }
 
+// Every element of C is some launch's, once, and every launch reads the rows of A and B that go with its part: products of more rows or columns than one grid has places for.
+static void sizes_beyond_a_grid() {
+    struct { int64_t m, n, k; } sizes[] = {{1, (1ll << 29) + 5, 256}, {16, (1ll << 28) + 77, 8192}, {1, (1ll << 31) - 1, 100}, {5000000, 3, 0}, {17, (1ll << 30) + 9, 0}, {(1ll << 31) - 1, 1, 0},
+                   {5000000, 70, 1ll << 25}, {3, 5, 0}, {40, 40, 1ll << 25}};
+    for (const auto &s : sizes)
+        for (int dtype : {int(CKPT_BF16), int(CKPT_F32)}) {
+            const uint64_t size = dtype == CKPT_F32 ? 4 : 2;
+            ckpt_mx_matrix a, b;
+            REQUIRE(ckpt_mx_layout(CKPT_MXFP4, s.m, s.k, &a) == CKPT_OK && ckpt_mx_layout(CKPT_MXFP4, s.n, s.k, &b) == CKPT_OK);
+            for (ckpt_mx_matrix *x : {&a, &b})
+                if (s.k) {
+                    x->codes = allocate(x->rows * x->code_pitch);
+                    x->scales = allocate(x->rows * x->scale_pitch);
+                }
+            const int64_t ldc = s.n + 3;
+            unsigned char *c = static_cast<unsigned char *>(allocate((s.m * ldc) * size));
+            launches.clear();
+            first_argument_bytes = sizeof(dsllm::GemmArgs);
+            const int rc = ckpt_mx_gemm(&a, &b, c, dtype, ldc, 0, nullptr, 0, nullptr);
+            printf("# %lld x %lld x %lld, %llu bytes an element: %d, %zu launches\n", (long long)s.m, (long long)s.n, (long long)s.k, (unsigned long long)size, rc, launches.size());
+            REQUIRE(rc == CKPT_OK && !launches.empty());
+            uint64_t covered = 0;
+            std::vector<std::pair<uint64_t, std::pair<int64_t, int64_t>>> places;
+            for (const Launch &l : launches) {
+                dsllm::GemmArgs p;
+                memcpy(&p, l.first.data(), sizeof p);
+                const uint64_t at = (static_cast<unsigned char *>(p.c) - c) / size, row = at / ldc, col = at % ldc;
+                REQUIRE(p.m > 0 && p.n > 0 && int64_t(row) + p.m <= s.m && int64_t(col) + p.n <= s.n && p.ldc == ldc);
+                REQUIRE(p.a == static_cast<uint8_t *>(a.codes) + row * a.code_pitch && p.a_scale == static_cast<uint8_t *>(a.scales) + row * a.scale_pitch);
+                REQUIRE(p.b == static_cast<uint8_t *>(b.codes) + col * b.code_pitch && p.b_scale == static_cast<uint8_t *>(b.scales) + col * b.scale_pitch);
+                for (const auto &q : places) REQUIRE(q.first != at);
+                places.push_back({at, {p.m, p.n}});
+                covered += uint64_t(p.m) * p.n;
+                if (l.kernel.find("few") != std::string::npos) REQUIRE(l.grid.x == uint64_t(p.n + 15) / 16 && l.grid.y == 1);
+                else if (l.kernel.find("long") != std::string::npos) REQUIRE(l.grid.x == uint64_t(p.n + 63) / 64 && l.grid.y == uint64_t(p.m + 63) / 64);
+                else REQUIRE(launches.size() == 1);
+            }
+            REQUIRE(covered == uint64_t(s.m) * s.n);
+            allocations.clear();
+        }
+}
+
 int main(int argc, char **argv) {
     const std::string what = argc > 1 ? argv[1] : "";
     if (what == "destroy") destroy_on_another_device();
+    else if (what == "grids") sizes_beyond_a_grid();
     else return 2;
     printf("ok\n");
 }

@@ -17,17 +17,16 @@ def program(tmp_path_factory):
         pytest.skip("hipcc not present")
     d = tmp_path_factory.mktemp("train_calls")
     objects = []
-    for f in ("optim", "mx_quantize", "mx_gemm"):
-        objects.append(str(d / (f + ".o")))
-        subprocess.run([HIPCC, "-x", "hip", "--cuda-host-only", "-c", os.path.join(build.CSRC, f + ".hip"), "-o", objects[-1]] + build.HIPCC_FLAGS, check=True, capture_output=True)
+    for f in [os.path.join(build.CSRC, f) for f in ("optim.hip", "mx_quantize.hip", "mx_gemm.hip")] + [os.path.join(ROOT, "tests", "emu", "train_calls.cpp")]:
+        objects.append(str(d / (os.path.basename(f) + ".o")))
+        subprocess.run([HIPCC, "-x", "hip", "--cuda-host-only", "-c", f, "-o", objects[-1]] + build.HIPCC_FLAGS, check=True, capture_output=True)
     exe = str(d / "train_calls")
     # the device code that the objects would register is not there, and not asked for
-    subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-no-pie", "-Wl,--unresolved-symbols=ignore-all", "-o", exe,
-                    os.path.join(ROOT, "tests", "emu", "train_calls.cpp")] + objects, check=True)
+    subprocess.run(["g++", "-no-pie", "-Wl,--unresolved-symbols=ignore-all", "-o", exe] + objects, check=True)
     return exe
 
 
-@pytest.mark.parametrize("what", ["destroy"])
+@pytest.mark.parametrize("what", ["destroy", "grids"])
 def test_calls(program, what):
     r = subprocess.run([program, what], capture_output=True, text=True, timeout=60)
-    assert r.returncode == 0 and r.stdout == "ok\n", r.stdout + r.stderr
+    assert r.returncode == 0 and r.stdout.endswith("ok\n"), r.stdout + r.stderr
