@@ -459,12 +459,16 @@ class Optimizer:
     """One ckpt_optim. tensors: iterable of dicts with the fields of ckpt_optim_tensor without the "dev_" prefix (numel and
     grad; master, m, v and, as the configuration asks for them, param, m_scale and v_scale; weight_decay)."""
 
+    _FIELDS = {name.removeprefix("dev_"): name for name, _ in ckpt_optim_tensor._fields_}
+
     def __init__(self, tensors, grad_dtype=CKPT_BF16, param_dtype=CKPT_BF16, state_bits=32):
         tensors = list(tensors)
         arr = (ckpt_optim_tensor * max(1, len(tensors)))()
         for k, t in enumerate(tensors):
             for name, value in t.items():
-                setattr(arr[k], name if name in ("numel", "weight_decay") else "dev_" + name, value)
+                if name not in self._FIELDS:
+                    raise TypeError(f"tensor {k}: unknown field {name!r}")
+                setattr(arr[k], self._FIELDS[name], value)
         cfg = ckpt_optim_config(grad_dtype, param_dtype, state_bits, 0)
         self._h = _vp()
         _check(lib.ckpt_optim_create(arr, len(tensors), C.byref(cfg), C.byref(self._h)))

@@ -74,3 +74,10 @@ def test_rows_draw_random_numbers_of_their_own():
     a = to.bits16(7, 3, 6)
     assert np.array_equal(a.reshape(-1)[:6], to.bits16(7, 1, 6)[0]) and np.array_equal(a[1], to.bits16(9, 1, 6)[0])
     assert a.min() >= 0 and a.max() < 65536
+
+
+def test_an_unknown_field_of_a_tensor_is_refused():
+    """A misspelt weight_decay would otherwise be 0."""
+    for tensor in (dict(numel=4, grad=0, weight_deacy=0.1), dict(numel=4, dev_grad=0)):
+        with pytest.raises(TypeError, match="weight_deacy|dev_grad"):
+            B.Optimizer([tensor])
