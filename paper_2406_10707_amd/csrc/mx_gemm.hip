@@ -12,10 +12,6 @@
 
 using namespace dsllm;
 
-namespace dsllm {
-const char *wrong_mx_matrix(const ckpt_mx_matrix *m, DeviceRanges &ranges);
-}
-
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));

@@ -6,10 +6,6 @@
 
 using namespace dsllm;
 
-namespace dsllm {
-const char *wrong_mx_matrix(const ckpt_mx_matrix *m, DeviceRanges &ranges);
-}
-
 namespace {
 
 struct RowArgs {
@@ -299,7 +295,6 @@ int dequantize(const ckpt_mx_matrix *m, void *dst, int32_t dtype, int64_t ld, hi
 
 }  // namespace
 
-// nullptr if the matrix is well formed and its rows are device memory
 const char *dsllm::wrong_mx_matrix(const ckpt_mx_matrix *m, DeviceRanges &ranges) {
     if (m->format != CKPT_MXFP4 && m->format != CKPT_MXFP8) return "format must be CKPT_MXFP4 or CKPT_MXFP8";
     if (m->reserved) return "reserved field not zero";

@@ -17,7 +17,6 @@ struct TensorEntry {
     uint8_t *param;
     float *master;
     uint8_t *m, *v, *m_scale, *v_scale;
-    uint64_t numel;
     uint64_t first_block;      // blocks of 32 of all tensors before it
     double weight_decay;
 };
@@ -83,11 +82,10 @@ template <int GRAD, uint32_t PIECE>
 __device__ __forceinline__ void load_piece(f32x4 *v, const uint8_t *p) {
     if constexpr (PIECE == 1) v[0] = load4<GRAD>(p);
     else {
-        typedef typename Element<GRAD>::one eight __attribute__((ext_vector_type(8)));
-        typedef eight eight_bytealigned __attribute__((aligned(1)));
-        const eight e = __builtin_nontemporal_load((const eight_bytealigned DSLLM_GLOBAL *)p);
-        v[0] = __builtin_convertvector(__builtin_shufflevector(e, e, 0, 1, 2, 3), f32x4);
-        v[1] = __builtin_convertvector(__builtin_shufflevector(e, e, 4, 5, 6, 7), f32x4);
+        Eight<GRAD> e;
+        e.load(p);
+        v[0] = __builtin_convertvector(e.lo, f32x4);
+        v[1] = __builtin_convertvector(e.hi, f32x4);
     }
 }
 
@@ -348,7 +346,7 @@ int create(const ckpt_optim_tensor *tensors, size_t n, const ckpt_optim_config *
         }
         if (!(fabs(t.weight_decay) <= 1e30)) return bad("weight_decay", "not a finite number");
         entries[k] = TensorEntry{static_cast<const uint8_t *>(t.dev_grad), static_cast<uint8_t *>(t.dev_param), t.dev_master, static_cast<uint8_t *>(t.dev_m),
-                                 static_cast<uint8_t *>(t.dev_v), static_cast<uint8_t *>(t.dev_m_scale), static_cast<uint8_t *>(t.dev_v_scale), t.numel, blocks, t.weight_decay};
+                                 static_cast<uint8_t *>(t.dev_v), static_cast<uint8_t *>(t.dev_m_scale), static_cast<uint8_t *>(t.dev_v_scale), blocks, t.weight_decay};
         o->numels.push_back(t.numel);
         blocks += (t.numel + 31) / 32;
         n_spans += (t.numel + kSpan - 1) / kSpan;

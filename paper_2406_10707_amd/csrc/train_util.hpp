@@ -61,6 +61,9 @@ public:
     }
 };
 
+// nullptr if the matrix is well formed and its rows are device memory, else what is wrong
+const char *wrong_mx_matrix(const ckpt_mx_matrix *m, DeviceRanges &ranges);
+
 inline uint32_t element_bytes(int32_t dtype) { return dtype == CKPT_F32 ? 4 : dtype == CKPT_BF16 || dtype == CKPT_F16 ? 2 : 0; }
 
 // ------------------------------------------------------------------ random bits (ckpt_proxy.h: mix)
