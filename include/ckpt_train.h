@@ -39,8 +39,8 @@ typedef enum { CKPT_ROUND_NEAREST = 0, CKPT_ROUND_STOCHASTIC = 1,
 /* rows x cols elements. Row r: codes at codes + r * code_pitch, scales at scales + r * scale_pitch.
  * MXFP4: code_pitch a multiple of 128 that holds cols / 2 bytes, scale_pitch a multiple of 16 that holds a byte for each
  * block of the pitch (code_pitch / 16), both addresses 16-byte aligned; what a row has behind its last element is zero
- * (ckpt_mx_quantize writes it so, ckpt_mx_gemm relies on it). MXFP8: pitches of at least cols and ceil(cols / 32) bytes.
- * Rows of a matrix may not overlap. */
+ * (ckpt_mx_quantize writes it so, ckpt_mx_gemm relies on it). MXFP8: pitches of at least cols and ceil(cols / 32) bytes; ckpt_mx_quantize
+ * writes all of a row's pitch here too, zeros behind its last element. Rows of a matrix may not overlap. */
 typedef struct {
     int32_t format;        /* ckpt_mx_format */
     int32_t reserved;      /* must be zero */

@@ -69,7 +69,7 @@ __device__ __forceinline__ u32x4 sum_of_sixteen_bytes(u32x4 sum, u32x4 old) {
 // once every wave has read its second half's fragments the stage is free and the loads of step + 2 into it start; three quarters into the step those of
 // step + 1 have landed for all. (Four steps in LDS: the loads are those of step + 4.) Tiles of more than 32 accumulators a wave name them as AGPRs in the instruction's own operands.
 //
-// 8192^3 takes 237 us = 4640 TFLOP/s with 256 x 256 tiles (gemm_long_kernel 3590): a step 2670 cycles, of which the matrix instructions are 2048, at 1.73 GHz, which the power allows (2.1 GHz
+// 8192^3 takes 226 to 254 us = 4.3 to 4.9 PFLOP/s with 256 x 256 tiles, from card to card (gemm_long_kernel 3590 us); at 237: a step 2670 cycles, of which the matrix instructions are 2048, at 1.73 GHz, which the power allows (2.1 GHz
 // without the panels' loads and reads); some 7000 cycles in front of a tile's 32 steps (the first loads of all waves) and 9000 behind them (the stores of C). Scales fetched 16 bytes a row and step cost 14 us
 // more, scales read from LDS at addresses of 2 bytes 150, pieces 2 q + h without the rotation (two lanes a bank) 15.
 template <int WM, int WN, int TM, int TN, int STAGES, int READS, int LOAD_EVERY, int OUT>
@@ -207,7 +207,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs &p, const TileOrde
     const int64_t part = blockIdx.y * p.c_split;
     if (p.vector && row + BM <= p.m && col + BN <= p.n) {
         // A whole tile goes through LDS, which is free now, so that a store is whole lines of C by neighbouring lanes (straight from the registers neighbouring lanes have different rows): 16384 x 16384 x 4096
-        // 614 -> 573 us, 8192^3 to f32 275 -> 268, 2304 x 768 x 8190 added to f32 17.7 -> 17.1, 1000 x 2304 x 768 to f32 6.6 -> 6.1, 8192^3 to bf16 even, 4096^3 36.2 -> 36.7. A wave has a part of
+        // 614 -> 573 us, 8192^3 to f32 275 -> 268 (other cards 254 and 273), 2304 x 768 x 8190 added to f32 17.7 -> 17.1, 1000 x 2304 x 768 to f32 6.6 -> 6.1, 8192^3 to bf16 even, 4096^3 36.2 -> 36.7. A wave has a part of
         // its own, rows of CP pieces of 16 bytes, of which CH are used; piece p of row r lies at place p ^ f(r). Few instructions a store: with the bounds of each beside it this was 40 KB of
         // code that every block fetched anew.
         constexpr int CH = OUT == CKPT_F32 ? 4 * TN : 2 * TN, CP = CH <= 4 ? 4 : CH <= 8 ? 8 : CH <= 16 ? 16 : 32, SHIFT = CP >= 16 ? 0 : CP == 8 ? 1 : 2, MASK = CP >= 16 ? 15 : CP - 1;
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(256, TOGETHER) void gemm_tile_kernel(GemmArgs p, Ti
 // of B, 16 of A, whose last is repeated where there are fewer; in the scales' window rows 16 to 31 are A's). Addresses are 64-bit ones.
 //
 // One token, launched in a row: 16384 x 16384 26 us = 5.4 TB/s (64 x 64 tiles 31), 4096 x 16384 8.2 (tiles 15.2, in four parts 10.9), 11008 x 4096 5.9 with two waves (four 6.4, tiles 6.1); below that the
-// launches are what counts (4.5 us). Fragments read straight from memory took 33, 11.7 and 7.4: sixteen lines a request.
+// launches are what counts (4.5 us). Sixteen rows: 27.5, 8.8, 5.9. Fragments read straight from memory took 33, 11.7 and 7.4: sixteen lines a request.
 template <int WAVES, int OUT>
 __global__ __launch_bounds__(64 * WAVES) void gemm_few_kernel(GemmArgs p) {
     constexpr int STEP = 2 * 16 * 128, SCALES = 32 * 32, WAVE = 4 * STEP + 2 * SCALES;

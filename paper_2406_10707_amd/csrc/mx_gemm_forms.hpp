@@ -4,8 +4,9 @@
 
 namespace dsllm {
 
-// A form's tile, how many of its blocks share a compute unit, and what it costs in us, fitted to 20 products from 300 x 300 x 300 to 8192^3 (mean 0.4 % over the
-// best form of each, at most 4 %): a step of 256 values of K with 1, 2, 3 blocks on the unit, and what a block takes besides.
+// A form's tile, how many of its blocks share a compute unit, and what it costs, fitted to 20 products from 300 x 300 x 300 to 8192^3 so that the forms of each come out in their order (the choice is
+// in the mean 0.4 % over the best form, at most 4 %): a step of 256 values of K with 1, 2, 3 blocks on the unit, and what a block takes besides. About microseconds, but no prediction of a time: 8192^3
+// is 202 here and takes 226 to 254.
 struct MxGemmForm {
     const char *name;
     uint32_t bm, bn, together;
@@ -24,7 +25,7 @@ constexpr MxGemmForm kMxGemmForms[] = {
 };
 constexpr int kMxGemmFormCount = sizeof(kMxGemmForms) / sizeof(kMxGemmForms[0]);
 constexpr uint32_t kComputeUnits = 256;
-constexpr double kJoin = 4.5, kJoinBytes = 5e6;      // us; bytes a us
+constexpr double kJoin = 4.5, kJoinBytes = 5e6;      // what the join costs besides; bytes a unit of cost
 
 // `splits` blocks share a tile, each with a part of K.
 inline double mx_gemm_cost(const MxGemmForm &f, uint64_t m, uint64_t n, uint64_t steps, uint32_t splits, bool f32_out) {
@@ -41,7 +42,8 @@ inline uint64_t mx_gemm_part_bytes(uint64_t m, uint64_t n) { return m * mx_gemm_
 inline uint32_t mx_gemm_steps_a_split(uint32_t steps, uint32_t splits) { return ((steps + splits - 1) / splits + 3) / 4 * 4; }
 
 // Up to sixteen rows of A have a kernel of their own: its waves for each 16 rows of B, 0 for other products. Two where K is up to 4096 (11008 x 4096 5.9 us, with four 6.4), else four (16384 x 16384
-// 26.2, with two 27.9, with eight 29.5).
+// 26.2, with two 27.9, with eight 29.5). However few rows B has: 16 x 64 x 16384 4.6 (the tiles in parts of K 9.0), 16 x 256 x 65536 13.1 (12.4), 1 x 16 x 65536 9.9 (10.6); only beyond do parts
+// pay (1 x 16 x 262144 33.7, in parts 17.8).
 inline uint32_t mx_gemm_few_waves(uint64_t m, uint32_t steps) { return m > 16 ? 0 : steps <= 16 ? 2 : 4; }
 
 struct MxGemmChoice { int form; uint32_t splits; };

@@ -31,7 +31,8 @@ __device__ __forceinline__ uint32_t fp4_codes_of_eight(f32x4 lo, f32x4 hi, uint6
 }
 
 // A wave takes 1024 elements of a row in groups of 512, eight elements a lane; four lanes a block of 32. Bound by memory: 60 M f32 to 8 bits 52 us = 5.8 TB/s, 55 stochastically (three 64-bit products for
-// every four elements; with four elements a lane 48 and 59: its accesses are whole lines, but there is more to do for each), 45 M bf16 to 4 bits 22 us = 5.2 TB/s (four a lane 24, one group of them 27).
+// every four elements; with four elements a lane 48 and 59: its accesses are whole lines, but there is more to do for each), 45 M bf16 to 4 bits 22 us = 5.2 TB/s (four a lane 24, one group of them 27),
+// stochastically 35, from f32 37 and 43. Rows of fewer than 1024 elements leave lanes without work.
 constexpr uint32_t kGroups = 2, kRowPiece = 512 * kGroups;
 template <int SRC, int FORMAT, bool STOCHASTIC, bool NONZERO>
 __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
@@ -85,8 +86,9 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
 
 // A tile of 128 x 128 elements, to the columns' form and, with BY_ROW, to the rows' as well, 64 rows at a time: read once, 16 lanes a row, rounded by rows as it comes, put into LDS, and read
 // from there by columns while the other 64 rows are under way. In LDS the rows of the second 32 begin 32 words further round the banks: the 32 columns x 2 blocks of 32 rows that a wave reads at
-// once lie in 64 different ones. 45 M f32 to both forms 47 us = 4.8 TB/s (all 128 rows at a time, two blocks a unit instead of four: 52; by two kernels that each read src 100), bf16 34 us (four elements a lane: 37), f32
-// stochastically 68. Loads that stand under a condition, with the conversion to f32 beside them, are waited for one by one: bf16 took 83 us with them. What it writes beyond the two forms, a third more, is scales: four
+// once lie in 64 different ones; the counter all the same has conflicts in half of the cycles that LDS works, a tenth of the kernel's. 45 M f32 to both forms 47 to 52 us = 4.8 to 4.4 TB/s (all 128 rows at a
+// time, two blocks a unit instead of four: 52 beside 47; by two kernels that each read src 100), bf16 34 us (four elements a lane: 37), stochastically 68 to 70 and 65; by columns alone 42 and 25,
+// stochastically 47 and 39. Loads that stand under a condition, with the conversion to f32 beside them, are waited for one by one: bf16 took 83 us with them. What it writes beyond the two forms, a third more, is scales: four
 // bytes of 32 at a time, of two XCDs' L2 (runs of tiles for each XCD write less and take 1 to 8 % longer).
 struct TileArgs {
     RowArgs by_row, by_col;      // by_col: rows, cols are src's; codes, scales its transpose's
@@ -168,7 +170,8 @@ struct ValueArgs {
     uint64_t pieces;
 };
 
-// Eight elements a lane, 512 of a row a wave. Bound by memory: 45 M 4-bit values to bf16 17.3 us = 6.6 TB/s (more a lane is no faster).
+// Eight elements a lane, 512 of a row a wave. Bound by memory: 45 M 4-bit values to bf16 17.3 us = 6.6 TB/s (more a lane is no faster), 8-bit ones
+// 27 us; to f32, whose eight are two stores of half of every 32 bytes, 69 and 44.
 constexpr uint32_t kValuePiece = 512;
 template <int FORMAT, int DST>
 __global__ __launch_bounds__(256) void values_kernel(ValueArgs a) {

@@ -183,7 +183,8 @@ __device__ __forceinline__ f32x4 updated(f32x4 w, f32x4 m, f32x4 v, float keep, 
 // nine streams, and shared memory that nothing uses keeps the front narrower still where the grid is larger than the chip: 124 M elements with f32 gradients 609 us, with room for twelve waves to a
 // compute unit 570 = 6.5 TB/s, for seven 596 (two groups a lane: 620, 604, 592; blocks of four waves that loop over a span 665). 8-bit moments need more waves, or more a lane: 405 M
 // elements 1057 us with one group, with two 1084 and, with room for twenty waves, 1055 (twelve waves: 1760 and 1171). Stochastic rounding fills the vector units as well (98 % of their cycles with 80 instructions
-// an element): without the sign of v and with the least code by two integer instructions 1040 us, with spans that every block finds work in 1009 = 6.5 TB/s.
+// an element, 94 % now): without the sign of v and with the least code by two integer instructions 1040 us, with spans that every block finds work in 1009 on the same card; other cards 1045 to 1063 = 6.1
+// to 6.2 TB/s, to nearest 1051. Tensors without gaps have lines that two blocks write: 78 M elements with 8-bit moments 291 us, each at a multiple of 32 elements 229.
 constexpr unsigned kFreeBlocks = 256 * 36;
 constexpr uint32_t kSpansALaunch = 1u << 21;      // a grid has fewer than 2^32 work-items
 // A wave a block, GROUPS groups of four elements a lane, 256 elements apart: kSpan / (256 GROUPS) blocks for each of n_full spans, one for each of the pieces behind them (blocks that find nothing to do
