@@ -1,7 +1,8 @@
 /*
  * The operators of a training step around the shard that libdsllm_ckpt snapshots: the norm of all gradients with the
  * clipping factor, the AdamW step over the whole tensor list with moments in 32 or in 8 bits, block-scaled 4-bit and 8-bit
- * floating point (the OCP microscaling formats MXFP4 and MXFP8 E4M3), and the product of two MXFP4 matrices.
+ * floating point (the OCP microscaling formats MXFP4 and MXFP8 E4M3), the product of two MXFP4 matrices; linear layers in 8-bit floating point with
+ * a scale for each block of 128: conversion, product, the gated feed-forward block with its backward pass.
  *
  * Same conventions as ckpt.h: plain C ABI, "dev" pointers are device memory of the CURRENT HIP device, a stream argument
  * is a hipStream_t passed as void*, calls return a ckpt_status (0 = ok, negative = error) and never throw or abort,
@@ -73,6 +74,84 @@ int ckpt_mx_dequantize(const ckpt_mx_matrix *src, void *dst, int32_t dst_dtype, 
 int ckpt_mx_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes);
 int ckpt_mx_gemm(const ckpt_mx_matrix *a, const ckpt_mx_matrix *b, void *c, int32_t c_dtype, int64_t ldc, int32_t accumulate,
                  void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* ---- matrices in 8 bits with a scale for each block of 128 ----
+ *
+ * 128 consecutive elements of a row (block_rows 1: activations, gradients) or 128 x 128 elements (block_rows 128: weights, whose rows'
+ * and columns' forms then hold the same values) share a scale in f32. An element stands for code * scale.
+ *   CKPT_F8_E4M3  largest value 448, no infinities, 0x7F is NaN
+ *   CKPT_F8_E5M2  largest value 57344
+ * With amax the largest magnitude of a block, MOST the format's largest value and every operation rounded to f32: scale =
+ * max(amax / MOST, 2^-126), code = the nearest value, ties to the even code, of x * min(MOST / amax, 2^126). A block with an infinity or a
+ * NaN has the scale NaN and is NaN as a whole. What other programs have rounded by another rule is taken as it is. */
+typedef enum { CKPT_F8_E4M3 = 3, CKPT_F8_E5M2 = 4 } ckpt_f8_format;
+
+/* rows x cols elements, each a byte. Row r: codes at codes + r * code_pitch; code_pitch a multiple of 16 that holds cols rounded up to
+ * 128, codes 16-byte aligned; between cols and that multiple a row's codes are zero (every call here writes them so and relies on it), what
+ * the pitch has beyond is not touched. Half the columns of a wider matrix are such a matrix where they begin at a multiple of 128. Scales
+ * lie by blocks of columns, so that a product reads those of neighbouring rows at once: that of element (r, c) is
+ * scales[(c / 128) * scale_pitch + r / block_rows], scale_pitch at least ceil(rows / block_rows). Matrices that a call writes may not
+ * overlap what it reads. cols is at most 2^23 where a product contracts over them. */
+typedef struct {
+    int32_t format;        /* ckpt_f8_format */
+    int32_t block_rows;    /* 1 or 128 */
+    int64_t rows, cols;
+    void *codes;
+    uint64_t code_pitch;   /* bytes */
+    float *scales;
+    uint64_t scale_pitch;  /* scales */
+} ckpt_f8_matrix;
+
+/* Fills format, block_rows, rows, cols and the smallest pitches (that of the codes a multiple of 128); codes and scales are set to NULL. The caller
+ * allocates rows * code_pitch bytes and ceil(cols / 128) * scale_pitch scales. */
+int ckpt_f8_layout(int32_t format, int32_t block_rows, int64_t rows, int64_t cols, ckpt_f8_matrix *out);
+
+/* Rounds src, a row-major matrix of src_dtype (CKPT_F32, CKPT_BF16, CKPT_F16; aligned to its element) with `ld` elements from row to row, to by_row (rows x
+ * cols) and / or by_col (the transpose: cols x rows), in one pass over src. Either may be NULL; both have the same block_rows, not
+ * necessarily the same format unless block_rows is 128. */
+int ckpt_f8_quantize(const void *src, int32_t src_dtype, int64_t ld, const ckpt_f8_matrix *by_row, const ckpt_f8_matrix *by_col, void *stream);
+
+/* The transpose of a matrix that is held in 8 bits: an activation kept by rows from the forward pass, as the product for a weight's gradient contracts over it. With
+ * block_rows 1 the values are rounded anew, in blocks of 128 along src's rows; with block_rows 128 in both (and the same format) they stay as they are. */
+int ckpt_f8_columns(const ckpt_f8_matrix *src, const ckpt_f8_matrix *by_col, void *stream);
+
+/* The values that a matrix stands for, as a row-major matrix of dst_dtype with `ld` elements from row to row. */
+int ckpt_f8_dequantize(const ckpt_f8_matrix *src, void *dst, int32_t dst_dtype, int64_t ld, void *stream);
+
+/* C = A * B^T, or C += A * B^T with accumulate != 0. A is M x K, B is N x K, in either format and blocks of either kind; C is row-major, CKPT_BF16, CKPT_F16 or
+ * CKPT_F32, aligned to its element, `ldc` elements from row to row. The products of a block are summed on the matrix cores and,
+ * times both scales (whose product f32 has to hold), added in f32; one rounding at the end. For C in 16 bits and more than sixteen rows of A these sums are those of the 8-bit matrix instructions, which cut products
+ * more than 13 bits below the largest of eight; for C in f32, and for up to sixteen rows, they are sums in f32. A linear layer y = x W^T takes (x, W) forward, (dy, W by
+ * columns) for dx and (dy by columns, x by columns) for dW. Some sizes split K among blocks and need workspace: ckpt_f8_gemm_workspace bytes (16-byte
+ * aligned, contents do not matter, not shared by calls that may overlap); with less (or NULL) the call runs with fewer parts or unsplit.
+ * C must not overlap A, B or the workspace. */
+int ckpt_f8_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes);
+int ckpt_f8_gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t c_dtype, int64_t ldc, int32_t accumulate, void *workspace,
+                 uint64_t workspace_bytes, void *stream);
+
+/* ---- the gated feed-forward block ----
+ *
+ * h = act(x Wg^T) * (x Wu^T), y = h Wd^T: the last is ckpt_f8_gemm. Activations:
+ *   CKPT_GATE_SILU  act(g) = g / (1 + exp(-g))
+ *   CKPT_GATE_GELU  act(g) = g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
+typedef enum { CKPT_GATE_SILU = 1, CKPT_GATE_GELU = 2 } ckpt_gate;
+
+/* Both projections, the activation, the product and the rounding to 8 bits in one pass. x is tokens x hidden, w_gate and w_up are ffn x hidden (one format,
+ * blocks of one kind); gate, up and h are tokens x ffn, CKPT_F8_E4M3 with block_rows 1. gate and up are what the backward pass needs, rounded to 8
+ * bits (h is made of the values before that rounding); both NULL: nothing is kept, as in serving. Workspace as in ckpt_f8_gemm, for few tokens. */
+int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *bytes);
+int ckpt_gated_forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8_matrix *w_up, int32_t activation, const ckpt_f8_matrix *gate,
+                       const ckpt_f8_matrix *up, const ckpt_f8_matrix *h, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* What ckpt_gated_backward writes, each or NULL, all with block_rows 1, gradients in either format, h as CKPT_F8_E4M3: by rows (tokens x ffn) for dx = dgate Wg + dup Wu, by columns (ffn x tokens) for the weights' gradients. */
+typedef struct {
+    const ckpt_f8_matrix *dgate, *dup, *dgate_by_col, *dup_by_col, *h_by_col;
+} ckpt_gated_grads;
+
+/* dh = dy Wd, dgate = dh * up * act'(gate), dup = dh * act(gate), h = act(gate) * up, in one pass: dh is never stored. dy is tokens x hidden,
+ * w_down by columns ffn x hidden, gate and up tokens x ffn as the forward pass kept them (block_rows 1). */
+int ckpt_gated_backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down_by_col, const ckpt_f8_matrix *gate, const ckpt_f8_matrix *up,
+                        int32_t activation, const ckpt_gated_grads *grads, void *stream);
 
 /* ---- the update phase over a list of tensors ---- */
 

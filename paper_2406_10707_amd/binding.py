@@ -150,6 +150,15 @@ class ckpt_mx_matrix(C.Structure):
                 ("code_pitch", C.c_uint64), ("scales", C.c_void_p), ("scale_pitch", C.c_uint64)]
 
 
+class ckpt_f8_matrix(C.Structure):
+    _fields_ = [("format", C.c_int32), ("block_rows", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p),
+                ("code_pitch", C.c_uint64), ("scales", C.c_void_p), ("scale_pitch", C.c_uint64)]
+
+
+class ckpt_gated_grads(C.Structure):
+    _fields_ = [(name, C.POINTER(ckpt_f8_matrix)) for name in ("dgate", "dup", "dgate_by_col", "dup_by_col", "h_by_col")]
+
+
 class ckpt_optim_tensor(C.Structure):
     _fields_ = [("numel", C.c_uint64), ("dev_grad", C.c_void_p), ("dev_param", C.c_void_p), ("dev_master", C.c_void_p), ("dev_m", C.c_void_p),
                 ("dev_v", C.c_void_p), ("dev_m_scale", C.c_void_p), ("dev_v_scale", C.c_void_p), ("weight_decay", C.c_double)]
@@ -170,14 +179,25 @@ class ckpt_adamw_args(C.Structure):
 
 CKPT_MXFP4, CKPT_MXFP8 = 1, 2
 CKPT_ROUND_NEAREST, CKPT_ROUND_STOCHASTIC, CKPT_ROUND_NONZERO = 0, 1, 2
+CKPT_F8_E4M3, CKPT_F8_E5M2 = 3, 4
+CKPT_GATE_SILU, CKPT_GATE_GELU = 1, 2
 
-_i64, _mx = C.c_int64, C.POINTER(ckpt_mx_matrix)
+_i64, _mx, _f8 = C.c_int64, C.POINTER(ckpt_mx_matrix), C.POINTER(ckpt_f8_matrix)
 _TRAIN_SIGS = {      # include/ckpt_train.h
     "ckpt_mx_layout": (C.c_int, [_i32, _i64, _i64, _mx]),
     "ckpt_mx_quantize": (C.c_int, [_vp, _i32, _i64, _mx, _mx, _i32, _u64, _vp]),
     "ckpt_mx_dequantize": (C.c_int, [_mx, _vp, _i32, _i64, _vp]),
     "ckpt_mx_gemm_workspace": (C.c_int, [_i64, _i64, _i64, C.POINTER(_u64)]),
     "ckpt_mx_gemm": (C.c_int, [_mx, _mx, _vp, _i32, _i64, _i32, _vp, _u64, _vp]),
+    "ckpt_f8_layout": (C.c_int, [_i32, _i32, _i64, _i64, _f8]),
+    "ckpt_f8_quantize": (C.c_int, [_vp, _i32, _i64, _f8, _f8, _vp]),
+    "ckpt_f8_columns": (C.c_int, [_f8, _f8, _vp]),
+    "ckpt_f8_dequantize": (C.c_int, [_f8, _vp, _i32, _i64, _vp]),
+    "ckpt_f8_gemm_workspace": (C.c_int, [_i64, _i64, _i64, C.POINTER(_u64)]),
+    "ckpt_f8_gemm": (C.c_int, [_f8, _f8, _vp, _i32, _i64, _i32, _vp, _u64, _vp]),
+    "ckpt_gated_workspace": (C.c_int, [_i64, _i64, _i64, C.POINTER(_u64)]),
+    "ckpt_gated_forward": (C.c_int, [_f8, _f8, _f8, _i32, _f8, _f8, _f8, _vp, _u64, _vp]),
+    "ckpt_gated_backward": (C.c_int, [_f8, _f8, _f8, _f8, _i32, C.POINTER(ckpt_gated_grads), _vp]),
     "ckpt_optim_create": (C.c_int, [C.POINTER(ckpt_optim_tensor), C.c_size_t, C.POINTER(ckpt_optim_config), C.POINTER(_vp)]),
     "ckpt_optim_destroy": (C.c_int, [_vp]),
     "ckpt_optim_set_grads": (C.c_int, [_vp, C.POINTER(_vp), C.c_size_t, _vp]),
@@ -453,6 +473,62 @@ def mx_gemm_workspace(m, n, k):
 def mx_gemm(a, b, c, c_dtype, ldc, stream, accumulate=False, workspace=None, workspace_bytes=0):
     """ckpt_mx_gemm: C (+)= A B^T; a, b are ckpt_mx_matrix."""
     _check(lib.ckpt_mx_gemm(a, b, c, c_dtype, ldc, accumulate, workspace, workspace_bytes, stream))
+
+
+def f8_matrix(fmt, rows, cols, codes, code_pitch, scales, scale_pitch, block_rows=1):
+    """A ckpt_f8_matrix: device addresses of codes and scales, bytes from row to row of the codes, scales from block of columns to block of columns."""
+    return ckpt_f8_matrix(fmt, block_rows, rows, cols, codes, code_pitch, scales, scale_pitch)
+
+
+def f8_layout(fmt, rows, cols, block_rows=1):
+    """ckpt_f8_layout: (code_pitch, scale_pitch), the smallest ones; allocate rows * code_pitch bytes and 4 * ceil(cols / 128) * scale_pitch."""
+    out = ckpt_f8_matrix()
+    _check(lib.ckpt_f8_layout(fmt, block_rows, rows, cols, C.byref(out)))
+    return out.code_pitch, out.scale_pitch
+
+
+def f8_quantize(src, src_dtype, ld, by_row, by_col, stream):
+    """ckpt_f8_quantize: by_row, by_col are ckpt_f8_matrix or None."""
+    _check(lib.ckpt_f8_quantize(src, src_dtype, ld, by_row, by_col, stream))
+
+
+def f8_columns(src, by_col, stream):
+    """ckpt_f8_columns: by_col becomes the transpose of src."""
+    _check(lib.ckpt_f8_columns(src, by_col, stream))
+
+
+def f8_dequantize(src, dst, dst_dtype, ld, stream):
+    _check(lib.ckpt_f8_dequantize(src, dst, dst_dtype, ld, stream))
+
+
+def f8_gemm_workspace(m, n, k):
+    """ckpt_f8_gemm_workspace: bytes of workspace that a product of these sizes can use."""
+    out = _u64()
+    _check(lib.ckpt_f8_gemm_workspace(m, n, k, C.byref(out)))
+    return out.value
+
+
+def f8_gemm(a, b, c, c_dtype, ldc, stream, accumulate=False, workspace=None, workspace_bytes=0):
+    """ckpt_f8_gemm: C (+)= A B^T; a, b are ckpt_f8_matrix."""
+    _check(lib.ckpt_f8_gemm(a, b, c, c_dtype, ldc, accumulate, workspace, workspace_bytes, stream))
+
+
+def gated_workspace(tokens, ffn, hidden):
+    """ckpt_gated_workspace: bytes of workspace that a forward pass of these sizes can use."""
+    out = _u64()
+    _check(lib.ckpt_gated_workspace(tokens, ffn, hidden, C.byref(out)))
+    return out.value
+
+
+def gated_forward(x, w_gate, w_up, activation, stream, h, gate=None, up=None, workspace=None, workspace_bytes=0):
+    """ckpt_gated_forward: h, and what the backward pass needs of gate and up, of x and both weights; all are ckpt_f8_matrix."""
+    _check(lib.ckpt_gated_forward(x, w_gate, w_up, activation, gate, up, h, workspace, workspace_bytes, stream))
+
+
+def gated_backward(dy, w_down_by_col, gate, up, activation, stream, dgate=None, dup=None, dgate_by_col=None, dup_by_col=None, h_by_col=None):
+    """ckpt_gated_backward: those of the five that are given, of dy, Wd by columns and what the forward pass kept; all are ckpt_f8_matrix."""
+    grads = ckpt_gated_grads(*(C.pointer(m) if m is not None else None for m in (dgate, dup, dgate_by_col, dup_by_col, h_by_col)))
+    _check(lib.ckpt_gated_backward(dy, w_down_by_col, gate, up, activation, grads, stream))
 
 
 class Optimizer:

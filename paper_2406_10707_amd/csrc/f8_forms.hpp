@@ -1,0 +1,66 @@
+// Which form a product of two 8-bit matrices with a scale for each block of 128 takes, by its sizes alone (host only).
+#pragma once
+#include <stdint.h>
+
+namespace dsllm {
+
+// A form's tile, how many of its blocks share a compute unit, and what it costs: a step of 128 values of K with 1, 2 blocks on the unit (B's scales those of 128 x 128; those of single rows), and what a
+// block takes besides. About microseconds.
+struct F8Form {
+    const char *name;
+    uint32_t bm, bn, together;
+    double step[2], step_rows[2], block;
+    uint64_t tiles(uint64_t m, uint64_t n) const { return (m + bm - 1) / bm * ((n + bn - 1) / bn); }
+};
+constexpr F8Form kF8Forms[] = {
+    {"256x256", 256, 256, 1, {1.3, 0}, {1.5, 0}, 8.0},
+    {"128x128", 128, 128, 2, {0.45, 0.8}, {0.5, 0.9}, 4.0},
+    {"64x64", 64, 64, 2, {0.22, 0.4}, {0.22, 0.4}, 2.5},
+};
+constexpr int kF8FormCount = sizeof(kF8Forms) / sizeof(kF8Forms[0]);
+constexpr uint32_t kF8Units = 256;
+constexpr double kF8Join = 4.5, kF8JoinBytes = 5e6;      // what joining parts of K costs besides; bytes a unit of cost
+constexpr uint64_t kF8MostTiles = 1u << 22;              // of a launch
+
+inline uint32_t f8_steps(uint64_t k) { return uint32_t((k + 127) / 128); }
+
+inline double f8_cost(const F8Form &f, uint64_t m, uint64_t n, uint32_t steps, uint32_t splits, bool rows) {
+    const uint64_t blocks = f.tiles(m, n) * splits, at_once = kF8Units * f.together, full = blocks / at_once, rest = blocks % at_once;
+    const double *step = rows ? f.step_rows : f.step;
+    double t = double(full) * (double(steps) * step[f.together - 1] + f.block);
+    if (rest) t += double(steps) * step[(rest + kF8Units - 1) / kF8Units - 1] + f.block;
+    return t;
+}
+
+// Parts of K lie one behind the other in the workspace, as f32 rows of whole 16 bytes.
+inline uint64_t f8_part_pitch(uint64_t n) { return (n + 3) / 4 * 4; }
+inline uint64_t f8_part_bytes(uint64_t m, uint64_t n) { return m * f8_part_pitch(n) * 4; }
+
+// Up to sixteen rows of A have a kernel of their own: its waves for each 16 rows of B, 0 for other products.
+inline uint32_t f8_few_waves(uint64_t m, uint32_t steps) { return m > 16 ? 0 : steps <= 32 ? 2 : 4; }
+
+struct F8Choice { int form; uint32_t splits; };
+
+// The cheapest form and number of parts whose parts fit the workspace. Joining the parts costs another launch and the way of the parts to memory and back.
+inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool rows, uint64_t workspace) {
+    const uint32_t steps = f8_steps(k);
+    F8Choice best{0, 1};
+    double least = 0;
+    for (int f = 0; f < kF8FormCount; f++)
+        for (uint32_t splits = 1; splits <= 16; splits *= 2) {
+            const uint32_t each = (steps + splits - 1) / splits;
+            if (splits > 1 && (uint64_t(each) * (splits - 1) >= steps || f8_part_bytes(m, n) > workspace / splits || kF8Forms[f].tiles(m, n) > kF8MostTiles)) break;
+            double t = f8_cost(kF8Forms[f], m, n, each, splits, rows);
+            if (splits > 1) t += kF8Join + double(f8_part_bytes(m, n)) * (2 * splits + 1) / kF8JoinBytes;
+            if ((f == 0 && splits == 1) || t < least) { best = F8Choice{f, splits}; least = t; }
+        }
+    return best;
+}
+
+// The gated block's forward pass: tiles of 256, 128 or 64 tokens by 128 columns of gate and of up.
+inline int gated_form(uint64_t tokens, uint64_t across) {
+    if ((tokens + 255) / 256 * across >= kF8Units) return 0;
+    return (tokens + 127) / 128 * across >= kF8Units ? 1 : 2;
+}
+
+}  // namespace dsllm

@@ -1,0 +1,129 @@
+// What products of 8-bit matrices with a scale for each block of 128 load, and to which places of LDS (f8_tile.hpp).
+#pragma once
+#include "gemm_tile.hpp"
+#include "kernel_util.hpp"
+
+namespace dsllm {
+
+struct F8Side {
+    const uint8_t *codes;
+    const float *scales;
+    uint64_t pitch, scale_pitch;
+    int64_t rows;
+    uint32_t shift;      // rows to a scale: 2^shift
+};
+// WM x WN waves, each computing (16 TM) x (16 TN) of the block's tile. TNG: fragments of B whose columns a lane holds one behind the other. STAGES steps of 128 values in LDS. PAIR: B's rows are those of two matrices, in turn
+// groups of 16 TNG rows of the one and of the other.
+//
+// LDS of a stage: a place of 128 bytes for each row of A and of B, in the order in which fragments read them: fragment i of a wave takes places 16 i to 16 i + 15 of the wave's, lane ar = lane mod 16 the place ar, which holds
+// row TM ar + i of A's wave tile, or row 4 TNG (ar / 4) + 4 j + ar mod 4 of a group of TNG fragments of B. Of place p, piece x (16 bytes) lies at x ^ f(p), f(p) = bits 1 to 3 of p, rotated: reads of neighbouring
+// places lie in different banks. The loads write LDS in lane order; both orders are made on the global side. Then a scale for each row of A and of B.
+template <int WM_, int WN_, int TM_, int TN_, int TNG_, int STAGES_, bool PAIR_>
+struct F8Shape {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, TNG = TNG_, STAGES = STAGES_;
+    static constexpr bool PAIR = PAIR_;
+    static constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, THREADS = 64 * NW;
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB + 1;      // a wave's loads of a step
+    static constexpr int CODES = (BM + BN) * 128, STAGE = CODES + 256 * NW, BYTES = STAGES * STAGE;
+    static_assert(LA * 8 * NW == BM && LB * 8 * NW == BN && TN % TNG == 0 && NW * 64 >= BM + BN && BM % 64 == 0, "loads divide among the waves");
+    static_assert(!PAIR || TN == 2 * TNG, "a wave has a group of each");
+};
+
+__device__ __forceinline__ uint32_t f8_rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
+
+template <class S>
+struct F8Loader {
+    __amdgpu_buffer_rsrc_t ra, rb[S::LB];
+    uint32_t off[S::LA + S::LB], wave;
+    const float *scale;
+    uint64_t scale_pitch;
+
+    // which of the two matrices, and which row behind the tile's first, the tile's row n of B is
+    static __device__ __forceinline__ uint32_t matrix_of(uint32_t n) { return S::PAIR ? (n / (16 * S::TNG)) & 1 : 0; }
+    static __device__ __forceinline__ uint32_t row_of(uint32_t n) { return S::PAIR ? n / (32 * S::TNG) * (16 * S::TNG) + n % (16 * S::TNG) : n; }
+
+    __device__ __forceinline__ F8Loader(const F8Side a, const F8Side b, const F8Side b2, uint32_t steps, int64_t row, int64_t col, int lane, uint32_t wave_) : wave(wave_) {
+        constexpr int ROWS_B = S::PAIR ? S::BN / 2 : S::BN;
+        const uint32_t last_a = uint32_t(min(a.rows - row, int64_t(S::BM)) - 1), last_b = uint32_t(min(b.rows - col, int64_t(ROWS_B)) - 1);      // rows past the end are the last row again
+        const uint32_t in_8 = lane >> 3, piece = 16 * ((lane & 7) ^ f8_rotated(((lane >> 4) & 3) | ((wave & 1) << 2)));
+        ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes + row * a.pitch), 0, last_a * uint32_t(a.pitch) + 128 * steps, 0x00020000);
+#pragma unroll
+        for (int c = 0; c < S::LA; c++) {
+            const uint32_t place = 8 * (S::NW * c + wave) + in_8, r = place / (16 * S::TM) * (16 * S::TM) + S::TM * (place % 16) + place / 16 % S::TM;
+            off[c] = min(r, last_a) * uint32_t(a.pitch) + piece;
+        }
+#pragma unroll
+        for (int c = 0; c < S::LB; c++) {
+            const uint32_t first = 8 * (S::NW * c + wave), place = first + in_8, ar = place % 16;
+            const uint32_t n = place / (16 * S::TNG) * (16 * S::TNG) + 4 * S::TNG * (ar / 4) + 4 * (place / 16 % S::TNG) + ar % 4;
+            const uint8_t *base = b.codes;
+            uint64_t pitch = b.pitch;
+            if (S::PAIR && matrix_of(first)) { base = b2.codes; pitch = b2.pitch; }
+            off[S::LA + c] = min(row_of(n), last_b) * uint32_t(pitch) + piece;
+            rb[c] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base + col * pitch), 0, last_b * uint32_t(pitch) + 128 * steps, 0x00020000);
+        }
+        const uint32_t slot = 64 * wave;      // of the wave's first lane: a wave's scales are all A's or all B's
+        if (slot < S::BM) {
+            scale = a.scales + ((row + min(slot + lane, last_a)) >> a.shift);
+            scale_pitch = a.scale_pitch;
+        } else {
+            const uint32_t n = min(slot - S::BM + lane, uint32_t(S::BN - 1));
+            scale = b.scales;
+            scale_pitch = b.scale_pitch;
+            if (S::PAIR && matrix_of(n)) { scale = b2.scales; scale_pitch = b2.scale_pitch; }
+            scale += (col + min(row_of(n), last_b)) >> b.shift;
+        }
+    }
+    // all loads of a step into a stage
+    __device__ __forceinline__ void issue(uint8_t *stage, uint32_t step) const {
+#pragma unroll
+        for (int c = 0; c < S::LA + S::LB; c++) issue(stage, step, c);
+        issue(stage, step, S::LA + S::LB);
+    }
+    __device__ __forceinline__ void issue(uint8_t *stage, uint32_t step, int c) const {
+        if (c < S::LA) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (DSLLM_LDS void *)(stage + 1024 * (S::NW * c + wave)), 16, off[c], 128 * step, 0, 0);
+        else if (c < S::LA + S::LB) __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[c < S::LA ? 0 : c - S::LA], (DSLLM_LDS void *)(stage + S::BM * 128 + 1024 * (S::NW * (c - S::LA) + wave)), 16, off[c], 128 * step, 0, 0);
+        else __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(scale + step * scale_pitch), (DSLLM_LDS void *)(stage + S::CODES + 256 * wave), 4, 0, 0);
+    }
+};
+
+// What a wave of a product of up to sixteen rows of A loads: 16 rows of A and of each of MATRICES, 128 bytes a row and step, four steps to a window. LDS of a wave: the places of four steps, of each A's 16, then the others'; then two windows'
+// scales, for each step 16 of A and 16 of each matrix. Rows past the end are the last row again; pieces of a place are permuted as in the tiles.
+template <int MATRICES>
+struct F8FewLoader {
+    static constexpr int SIDES = 1 + MATRICES, STEP = SIDES * 2048, SCALES = 4 * SIDES * 64, STEP_LOADS = 2 * SIDES, SCALE_LOADS = SIDES, WAVE = 4 * STEP + 2 * SCALES;
+    const uint8_t *from[STEP_LOADS];      // this lane's piece of the rows lane / 8 and that + 8 of each side
+    const float *scale_from[SCALE_LOADS];
+    uint32_t scale_step[SCALE_LOADS], steps;
+    uint64_t scale_pitch[SCALE_LOADS];
+
+    __device__ __forceinline__ F8FewLoader(const F8Side &a, const F8Side &b, const F8Side &b2, uint32_t steps_, int64_t n0, int lane) : steps(steps_) {
+#pragma unroll
+        for (int i = 0; i < STEP_LOADS; i++) {
+            const int r = 8 * (i & 1) + (lane >> 3);
+            const F8Side &side = i < 2 ? a : i < 4 ? b : b2;
+            from[i] = side.codes + min((i < 2 ? 0 : n0) + r, side.rows - 1) * side.pitch + 16 * ((lane & 7) ^ f8_rotated((r >> 1) & 7));
+        }
+#pragma unroll
+        for (int i = 0; i < SCALE_LOADS; i++) {      // scale 64 i + lane of a window: step, then side, then row
+            const uint32_t at = 64 * i + lane, which = at / 16 % SIDES;
+            const F8Side &side = which == 0 ? a : which == 1 ? b : b2;
+            scale_step[i] = at / (16 * SIDES);
+            scale_from[i] = side.scales + (min((which ? n0 : 0) + int64_t(at % 16), side.rows - 1) >> side.shift);
+            scale_pitch[i] = side.scale_pitch;
+        }
+    }
+    // steps past the end are the last again
+    __device__ __forceinline__ void issue_scales(uint8_t *mine, uint32_t window, uint32_t odd) const {
+#pragma unroll
+        for (int i = 0; i < SCALE_LOADS; i++)
+            __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(scale_from[i] + min(4 * window + scale_step[i], steps - 1) * scale_pitch[i]), (DSLLM_LDS void *)(mine + 4 * STEP + (odd & 1) * SCALES + 256 * i), 4, 0, 0);
+    }
+    __device__ __forceinline__ void issue_step(uint8_t *mine, uint32_t window, int s) const {
+        const uint64_t at = 128 * uint64_t(min(4 * window + s, steps - 1));
+#pragma unroll
+        for (int i = 0; i < STEP_LOADS; i++) __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(from[i] + at), (DSLLM_LDS void *)(mine + s * STEP + 1024 * i), 16, 0, 0);
+    }
+};
+
+}  // namespace dsllm

@@ -1,0 +1,327 @@
+// Conversion to matrices in 8 bits with a scale for each block of 128, their transposes, and back (include/ckpt_train.h).
+#include <algorithm>
+#include <type_traits>
+
+#include "f8_rows.hpp"
+
+using namespace dsllm;
+
+namespace {
+
+constexpr int kHeld = 0;      // a source that is itself held in 8 bits
+
+// ------------------------------------------------------------------ rows alone
+
+template <int SRC>
+__global__ __launch_bounds__(256) void f8_rows_kernel(F8Source src, F8Held to, uint32_t across) {
+    const uint32_t down = blockIdx.x / across;
+    f8_round_rows<SRC>(src, to, 16 * int64_t(down), 512 * int64_t(blockIdx.x - down * across));
+}
+
+// ------------------------------------------------------------------ tiles: columns, both forms, blocks of 128 x 128
+
+// Word i of four, each with four bytes, becomes the four words' bytes i.
+__device__ __forceinline__ u32x4 transposed(u32x4 v) {
+    const uint32_t ab_lo = __builtin_amdgcn_perm(v.y, v.x, 0x05010400), ab_hi = __builtin_amdgcn_perm(v.y, v.x, 0x07030602);      // x0 y0 x1 y1, x2 y2 x3 y3
+    const uint32_t cd_lo = __builtin_amdgcn_perm(v.w, v.z, 0x05010400), cd_hi = __builtin_amdgcn_perm(v.w, v.z, 0x07030602);
+    return u32x4{__builtin_amdgcn_perm(cd_lo, ab_lo, 0x05040100), __builtin_amdgcn_perm(cd_lo, ab_lo, 0x07060302), __builtin_amdgcn_perm(cd_hi, ab_hi, 0x05040100),
+                 __builtin_amdgcn_perm(cd_hi, ab_hi, 0x07060302)};
+}
+
+// A tile of 128 x 128 elements, which stays in registers: a thread has eight by eight of them, sixteen lanes across, four groups of eight rows a wave. The rows' largest values are found among sixteen lanes, the columns' among
+// a wave's four groups and, through LDS, the four waves. The columns' codes go through LDS as bytes (128 columns of 128, and 16 more so that neighbouring columns begin in different banks), so that a
+// store is whole lines. SQUARE: one scale for the tile, so that both forms have the same codes. Bound by memory.
+template <int SRC, bool BY_ROW, bool BY_COL, bool SQUARE>
+__global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_row, F8Held by_col, uint32_t across_tiles) {
+    constexpr bool HELD = SRC == kHeld, KEPT = HELD && SQUARE;      // KEPT: codes and scales move as they are
+    constexpr int PITCH = 128 + 16;
+    __shared__ __attribute__((aligned(16))) uint8_t turned[BY_COL ? 128 * PITCH : 16];
+    __shared__ uint32_t most_of_wave[4][128];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, across = threadIdx.x & 15, down = threadIdx.x >> 4;
+    const uint32_t tile_down = blockIdx.x / across_tiles, tile_across = blockIdx.x - tile_down * across_tiles;
+    const int64_t row0 = 128 * int64_t(tile_down) + 8 * down, col0 = 128 * int64_t(tile_across), col = col0 + 8 * across;
+    const bool whole = 128 * int64_t(tile_down) + 128 <= src.rows && col0 + 128 <= src.cols;      // loads without conditions: all are under way before the first is waited for
+    const uint32_t count = col < src.cols ? uint32_t(min(src.cols - col, int64_t(8))) : 0;
+    f32x4 lo[8], hi[8];
+    u32x2 codes[8];
+    if constexpr (HELD) {
+        const uint8_t *at = src.at + row0 * src.ld + col;      // a row's codes reach to a multiple of 128
+        float scale[8];
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) codes[i] = *(const u32x2 DSLLM_GLOBAL *)(at + i * src.ld);
+            if constexpr (!KEPT)
+#pragma unroll
+                for (int i = 0; i < 8; i++) scale[i] = ((const float DSLLM_GLOBAL *)src.scales)[tile_across * src.scale_pitch + row0 + i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                codes[i] = row0 + i < src.rows ? *(const u32x2 DSLLM_GLOBAL *)(at + i * src.ld) : u32x2{0, 0};
+                if constexpr (!KEPT) scale[i] = row0 + i < src.rows ? ((const float DSLLM_GLOBAL *)src.scales)[tile_across * src.scale_pitch + row0 + i] : 0;
+            }
+        }
+        if constexpr (!KEPT)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                lo[i] = f8_values(codes[i].x, src.e5m2) * scale[i];
+                hi[i] = f8_values(codes[i].y, src.e5m2) * scale[i];
+            }
+    } else {
+        constexpr uint32_t kBytes = sizeof(typename Element<SRC>::one);
+        const uint8_t *at = src.at + (row0 * src.ld + col) * kBytes;
+        Eight<SRC> x[8];
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i].load(at + i * src.ld * kBytes);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i].load_upto(at + i * src.ld * kBytes, row0 + i < src.rows ? count : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            lo[i] = __builtin_convertvector(x[i].lo, f32x4);
+            hi[i] = __builtin_convertvector(x[i].hi, f32x4);
+        }
+    }
+    // behind the last row and column zeros, whatever the block's scale
+    auto inside = [&](u32x2 c, int64_t left, uint32_t n) {
+        if (whole) return c;
+        const uint64_t kept = left <= 0 ? 0 : n >= 8 ? ~0ull : (1ull << (8 * n)) - 1;
+        return u32x2{c.x & uint32_t(kept), c.y & uint32_t(kept >> 32)};
+    };
+    uint32_t amax = 0;
+    float inverse = 0;
+    if constexpr (SQUARE && !KEPT) {
+        float largest = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) largest = larger(larger(largest, lo[i]), hi[i]);
+        amax = most_of_quarters(most_of_16(bits_of(largest)));
+        if (lane == 0) most_of_wave[wave][0] = amax;
+        __syncthreads();
+        amax = max(max(most_of_wave[0][0], most_of_wave[1][0]), max(most_of_wave[2][0], most_of_wave[3][0]));
+        const bool e5m2 = BY_ROW ? by_row.e5m2 : by_col.e5m2;
+        inverse = f8_inverse(amax, f8_most(e5m2));
+#pragma unroll
+        for (int i = 0; i < 8; i++) codes[i] = inside(u32x2{f8_codes(lo[i] * inverse, e5m2), f8_codes(hi[i] * inverse, e5m2)}, src.rows - row0 - i, count);
+        if (threadIdx.x == 0) {
+            const float scale = f8_scale(amax, f8_most(e5m2));
+            if constexpr (BY_ROW) ((float DSLLM_GLOBAL *)by_row.scales)[tile_across * by_row.scale_pitch + tile_down] = scale;
+            if constexpr (BY_COL) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + tile_across] = scale;
+        }
+    }
+    if constexpr (KEPT)
+        if (threadIdx.x == 0) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + tile_across] = ((const float DSLLM_GLOBAL *)src.scales)[tile_across * src.scale_pitch + tile_down];
+    if constexpr (BY_ROW) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            u32x2 c = codes[i];
+            if constexpr (!SQUARE) {
+                amax = most_of_16(bits_of(larger(larger(0, lo[i]), hi[i])));
+                inverse = f8_inverse(amax, f8_most(by_row.e5m2));
+                c = inside(u32x2{f8_codes(lo[i] * inverse, by_row.e5m2), f8_codes(hi[i] * inverse, by_row.e5m2)}, src.rows - row0 - i, count);
+                if (across == i && (whole || row0 + i < src.rows)) ((float DSLLM_GLOBAL *)by_row.scales)[tile_across * by_row.scale_pitch + row0 + i] = f8_scale(amax, f8_most(by_row.e5m2));
+            }
+            if (whole || row0 + i < src.rows) __builtin_nontemporal_store(c, (u32x2 DSLLM_GLOBAL *)(by_row.codes + (row0 + i) * by_row.code_pitch + col));
+        }
+    }
+    if constexpr (BY_COL) {
+        if constexpr (!SQUARE) {
+            uint32_t most[8];      // bits of magnitudes, which order like them
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                auto at = [&](int i) { return j < 4 ? lo[i][j & 3] : hi[i][j & 3]; };
+                most[j] = bits_of(larger(larger(0, f32x4{at(0), at(1), at(2), at(3)}), f32x4{at(4), at(5), at(6), at(7)}));
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                most[j] = most_of_quarters(most[j]);
+                if (lane < 16) most_of_wave[wave][8 * across + j] = most[j];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const uint32_t c = 8 * across + j;
+                most[j] = max(max(most_of_wave[0][c], most_of_wave[1][c]), max(most_of_wave[2][c], most_of_wave[3][c]));
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const float by = f8_inverse(most[j], f8_most(by_col.e5m2));
+                f32x4 a, b;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    a[i] = (j < 4 ? lo[i][j & 3] : hi[i][j & 3]) * by;
+                    b[i] = (j < 4 ? lo[i + 4][j & 3] : hi[i + 4][j & 3]) * by;
+                }
+                const u32x2 c = inside(u32x2{f8_codes(a, by_col.e5m2), f8_codes(b, by_col.e5m2)}, int64_t(count) - j, uint32_t(max(int64_t(0), min(src.rows - row0, int64_t(8)))));
+                *reinterpret_cast<u32x2 *>(turned + (8 * across + j) * PITCH + 8 * down) = c;
+                if (down == j && (whole || j < int(count))) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + col + j] = f8_scale(most[j], f8_most(by_col.e5m2));
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {      // columns 4 h to 4 h + 3
+                const u32x4 upper = transposed(u32x4{codes[0][h], codes[1][h], codes[2][h], codes[3][h]}), lower = transposed(u32x4{codes[4][h], codes[5][h], codes[6][h], codes[7][h]});
+#pragma unroll
+                for (int j = 0; j < 4; j++) *reinterpret_cast<u32x2 *>(turned + (8 * across + 4 * h + j) * PITCH + 8 * down) = u32x2{upper[j], lower[j]};
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t c = 32 * i + (threadIdx.x >> 3), piece = 16 * (threadIdx.x & 7);
+            if (whole || col0 + c < src.cols)
+                __builtin_nontemporal_store(*reinterpret_cast<const u32x4 *>(turned + c * PITCH + piece), (u32x4 DSLLM_GLOBAL *)(by_col.codes + (col0 + c) * by_col.code_pitch + 128 * uint64_t(tile_down) + piece));
+        }
+    }
+}
+
+// ------------------------------------------------------------------ values
+
+// Eight elements a lane, 512 of a row a wave. Bound by memory.
+template <int DST>
+__global__ __launch_bounds__(256) void f8_values_kernel(F8Held from, uint8_t *dst, uint64_t ld, uint32_t pieces) {
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t item = uint64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = item / pieces, col = (item - row * pieces) * 512 + 8 * lane;
+    if (row >= from.rows || col >= from.cols) return;
+    const float scale = ((const float DSLLM_GLOBAL *)from.scales)[(col / 128) * from.scale_pitch + (row >> from.shift)];
+    const u32x2 codes = *(const u32x2 DSLLM_GLOBAL *)(from.codes + row * from.code_pitch + col);
+    const f32x4 lo = f8_values(codes.x, from.e5m2) * scale, hi = f8_values(codes.y, from.e5m2) * scale;
+    uint8_t *at = dst + (row * ld + col) * sizeof(typename Element<DST>::one);
+    if (col + 8 <= from.cols) return store8<DST>(at, lo, hi);
+    store_upto4<DST>(at, lo, uint32_t(from.cols - col));
+    if (col + 4 < from.cols) store_upto4<DST>(at + 4 * sizeof(typename Element<DST>::one), hi, uint32_t(from.cols - col - 4));
+}
+
+// ------------------------------------------------------------------ host
+
+constexpr const char *kTooLarge = "the matrix takes more than 2^24 blocks of threads";
+bool fits_grid(uint64_t down, uint64_t across) { return down < 1u << 24 && across < 1u << 24 && down * across < 1u << 24; }
+
+template <int SRC>
+int launch_quantize(const F8Source &src, const F8Held &by_row, const F8Held &by_col, bool square, hipStream_t stream) {
+    if (!by_col.codes && !square) {
+        const uint64_t down = (uint64_t(src.rows) + 15) / 16, across = (uint64_t(src.cols) + 511) / 512;
+        if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooLarge);
+        hipLaunchKernelGGL(f8_rows_kernel<SRC>, dim3(unsigned(down * across)), dim3(256), 0, stream, src, by_row, uint32_t(across));
+        return launched();
+    }
+    const uint64_t down = (uint64_t(src.rows) + 127) / 128, across = (uint64_t(src.cols) + 127) / 128;
+    if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooLarge);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(down * across)), dim3(256), 0, stream, src, by_row, by_col, uint32_t(across)); };
+    if (square) !by_col.codes ? go(f8_tile_kernel<SRC, true, false, true>) : by_row.codes ? go(f8_tile_kernel<SRC, true, true, true>) : go(f8_tile_kernel<SRC, false, true, true>);
+    else by_row.codes ? go(f8_tile_kernel<SRC, true, true, false>) : go(f8_tile_kernel<SRC, false, true, false>);
+    return launched();
+}
+
+int quantize(const void *src, int32_t dtype, int64_t ld, const ckpt_f8_matrix *by_row, const ckpt_f8_matrix *by_col, hipStream_t stream) {
+    if (!by_row && !by_col) return refuse(CKPT_EINVAL, "neither by_row nor by_col");
+    const uint32_t bytes = element_bytes(dtype);
+    if (!bytes) return refuse(CKPT_EINVAL, "src_dtype must be CKPT_F32, CKPT_BF16 or CKPT_F16");
+    DeviceRanges ranges;
+    for (const ckpt_f8_matrix *m : {by_row, by_col})
+        if (m)
+            if (const char *why = wrong_f8_matrix(m, ranges)) return refuse(CKPT_EINVAL, std::string(m == by_row ? "by_row: " : "by_col: ") + why);
+    if (by_row && by_col) {
+        if (by_row->rows != by_col->cols || by_row->cols != by_col->rows) return refuse(CKPT_EINVAL, "by_col is not of the transpose's size");
+        if (by_row->block_rows != by_col->block_rows) return refuse(CKPT_EINVAL, "by_row and by_col differ in block_rows");
+        if (by_row->block_rows == 128 && by_row->format != by_col->format) return refuse(CKPT_EINVAL, "by_row and by_col differ in their format: with block_rows 128 they hold the same values");
+    }
+    const int64_t rows = by_row ? by_row->rows : by_col->cols, cols = by_row ? by_row->cols : by_col->rows;
+    if (rows == 0 || cols == 0) return CKPT_OK;
+    if (ld < cols || ld > (1ll << 48) / rows) return refuse(CKPT_EINVAL, "ld is smaller than a row, or the matrix too large");
+    if (uint64_t(src) % bytes) return refuse(CKPT_EINVAL, "src is not aligned to its element");
+    if (const char *why = ranges.wrong(src, (uint64_t(rows - 1) * ld + cols) * bytes)) return refuse(CKPT_EINVAL, std::string("src: ") + why);
+    const F8Source from{static_cast<const uint8_t *>(src), uint64_t(ld), rows, cols, nullptr, 0, 0};
+    const bool square = (by_row ? by_row : by_col)->block_rows == 128;
+    switch (dtype) {
+        case CKPT_F32: return launch_quantize<CKPT_F32>(from, F8Held(by_row), F8Held(by_col), square, stream);
+        case CKPT_BF16: return launch_quantize<CKPT_BF16>(from, F8Held(by_row), F8Held(by_col), square, stream);
+        default: return launch_quantize<CKPT_F16>(from, F8Held(by_row), F8Held(by_col), square, stream);
+    }
+}
+
+int columns(const ckpt_f8_matrix *src, const ckpt_f8_matrix *by_col, hipStream_t stream) {
+    if (!src || !by_col) return refuse(CKPT_EINVAL, "null argument");
+    DeviceRanges ranges;
+    if (const char *why = wrong_f8_matrix(src, ranges)) return refuse(CKPT_EINVAL, std::string("src: ") + why);
+    if (const char *why = wrong_f8_matrix(by_col, ranges)) return refuse(CKPT_EINVAL, std::string("by_col: ") + why);
+    if (src->rows != by_col->cols || src->cols != by_col->rows) return refuse(CKPT_EINVAL, "by_col is not of the transpose's size");
+    if (src->block_rows != by_col->block_rows) return refuse(CKPT_EINVAL, "src and by_col differ in block_rows");
+    if (src->block_rows == 128 && src->format != by_col->format) return refuse(CKPT_EINVAL, "src and by_col differ in their format: with block_rows 128 the values stay as they are");
+    if (src->rows == 0 || src->cols == 0) return CKPT_OK;
+    const F8Source from{static_cast<const uint8_t *>(src->codes), src->code_pitch, src->rows, src->cols, src->scales, src->scale_pitch, src->format == CKPT_F8_E5M2};
+    const uint64_t down = (uint64_t(src->rows) + 127) / 128, across = (uint64_t(src->cols) + 127) / 128;
+    if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooLarge);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(down * across)), dim3(256), 0, stream, from, F8Held(), F8Held(by_col), uint32_t(across)); };
+    src->block_rows == 128 ? go(f8_tile_kernel<kHeld, false, true, true>) : go(f8_tile_kernel<kHeld, false, true, false>);
+    return launched();
+}
+
+int dequantize(const ckpt_f8_matrix *m, void *dst, int32_t dtype, int64_t ld, hipStream_t stream) {
+    if (!m) return refuse(CKPT_EINVAL, "null argument");
+    const uint32_t bytes = element_bytes(dtype);
+    if (!bytes) return refuse(CKPT_EINVAL, "dst_dtype must be CKPT_F32, CKPT_BF16 or CKPT_F16");
+    DeviceRanges ranges;
+    if (const char *why = wrong_f8_matrix(m, ranges)) return refuse(CKPT_EINVAL, std::string("src: ") + why);
+    if (m->rows == 0 || m->cols == 0) return CKPT_OK;
+    if (ld < m->cols || ld > (1ll << 48) / m->rows) return refuse(CKPT_EINVAL, "ld is smaller than a row, or the matrix too large");
+    if (uint64_t(dst) % bytes) return refuse(CKPT_EINVAL, "dst is not aligned to its element");
+    if (const char *why = ranges.wrong(dst, (uint64_t(m->rows - 1) * ld + m->cols) * bytes)) return refuse(CKPT_EINVAL, std::string("dst: ") + why);
+    const uint64_t pieces = (uint64_t(m->cols) + 511) / 512;
+    if (uint64_t(m->rows) > 1ull << 26 || !fits_grid((m->rows + 3) / 4, pieces)) return refuse(CKPT_EINVAL, kTooLarge);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((m->rows * pieces + 3) / 4)), dim3(256), 0, stream, F8Held(m), static_cast<uint8_t *>(dst), uint64_t(ld), uint32_t(pieces)); };
+    switch (dtype) {
+        case CKPT_F32: go(f8_values_kernel<CKPT_F32>); break;
+        case CKPT_BF16: go(f8_values_kernel<CKPT_BF16>); break;
+        default: go(f8_values_kernel<CKPT_F16>);
+    }
+    return launched();
+}
+
+}  // namespace
+
+const char *dsllm::wrong_f8_matrix(const ckpt_f8_matrix *m, DeviceRanges &ranges) {
+    if (m->format != CKPT_F8_E4M3 && m->format != CKPT_F8_E5M2) return "format must be CKPT_F8_E4M3 or CKPT_F8_E5M2";
+    if (m->block_rows != 1 && m->block_rows != 128) return "block_rows must be 1 or 128";
+    if (m->rows < 0 || m->cols < 0 || m->rows > 1ll << 40 || m->cols > 1ll << 40) return "rows or cols out of range";
+    if (m->rows == 0 || m->cols == 0) return nullptr;
+    const uint64_t rows = uint64_t(m->rows), padded = f8_padded(m->cols), scale_rows = (rows + m->block_rows - 1) / m->block_rows;
+    if (m->code_pitch % 16 || uint64_t(m->codes) % 16 || uint64_t(m->scales) % 4) return "a pitch and an address of 16 bytes are wanted for the codes, one of 4 for the scales";
+    if (m->code_pitch < padded || m->scale_pitch < scale_rows) return "a pitch is smaller than a row, or than a block of columns";
+    if (m->code_pitch > (1ull << 48) / rows || m->scale_pitch > (1ull << 48) / padded) return "the matrix is too large";
+    if (const char *why = ranges.wrong(m->codes, (rows - 1) * m->code_pitch + padded)) return why;
+    return ranges.wrong(m->scales, 4 * ((padded / 128 - 1) * m->scale_pitch + scale_rows));
+}
+
+extern "C" {
+
+int ckpt_f8_layout(int32_t format, int32_t block_rows, int64_t rows, int64_t cols, ckpt_f8_matrix *out) {
+    return at_c_entry([&] {
+        if (!out) return refuse(CKPT_EINVAL, "null argument");
+        *out = ckpt_f8_matrix{};
+        if (format != CKPT_F8_E4M3 && format != CKPT_F8_E5M2) return refuse(CKPT_EINVAL, "format must be CKPT_F8_E4M3 or CKPT_F8_E5M2");
+        if (block_rows != 1 && block_rows != 128) return refuse(CKPT_EINVAL, "block_rows must be 1 or 128");
+        if (rows < 0 || cols < 0 || rows > 1ll << 40 || cols > 1ll << 40) return refuse(CKPT_EINVAL, "rows or cols out of range");
+        out->format = format;
+        out->block_rows = block_rows;
+        out->rows = rows;
+        out->cols = cols;
+        out->code_pitch = f8_padded(cols);
+        out->scale_pitch = (uint64_t(rows) + block_rows - 1) / block_rows;
+        return int(CKPT_OK);
+    });
+}
+
+int ckpt_f8_quantize(const void *src, int32_t src_dtype, int64_t ld, const ckpt_f8_matrix *by_row, const ckpt_f8_matrix *by_col, void *stream) {
+    return at_c_entry([&] { return quantize(src, src_dtype, ld, by_row, by_col, static_cast<hipStream_t>(stream)); });
+}
+
+int ckpt_f8_columns(const ckpt_f8_matrix *src, const ckpt_f8_matrix *by_col, void *stream) {
+    return at_c_entry([&] { return columns(src, by_col, static_cast<hipStream_t>(stream)); });
+}
+
+int ckpt_f8_dequantize(const ckpt_f8_matrix *src, void *dst, int32_t dst_dtype, int64_t ld, void *stream) {
+    return at_c_entry([&] { return dequantize(src, dst, dst_dtype, ld, static_cast<hipStream_t>(stream)); });
+}
+
+}  // extern "C"
