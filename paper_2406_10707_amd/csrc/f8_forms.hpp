@@ -4,31 +4,36 @@
 
 namespace dsllm {
 
-// A form's tile, how many of its blocks share a compute unit, and what it costs: a step of 128 values of K with 1, 2 blocks on the unit (B's scales those of 128 x 128; those of single rows), and what a
-// block takes besides. About microseconds.
+// A form's tile, how many of its blocks share a compute unit, and what it costs, about microseconds, fitted to 1200 times of 26 products from 300 x 2050 x 768 to 11008 x 4096 x 8192: a step of 128 values of K with blocks on every unit (and in
+// every round but the last) or, of forms whose blocks share a unit, with one on it; what a block takes besides, with C in 16 bits or in f32. Steps for the two kinds of sums (8-bit instructions, bf16) and of B's scales (of 128 x 128,
+// of single rows). The choice is in the mean 1 % over the best
+// form, at most 8 %.
 struct F8Form {
     const char *name;
     uint32_t bm, bn, together;
-    double step[2], step_rows[2], block;
+    double step[4][2], block[2];      // [2 wide + rows]: of the last round with up to one block a unit, of others
     uint64_t tiles(uint64_t m, uint64_t n) const { return (m + bm - 1) / bm * ((n + bn - 1) / bn); }
 };
+// Sums of the 8-bit instructions with scales of single rows do not fit the registers of a 64 x 128 wave (they spill: 8192^3 650 us, with 256 x 128 tiles 555).
+constexpr double kF8Never = 1e9;
 constexpr F8Form kF8Forms[] = {
-    {"256x256", 256, 256, 1, {1.3, 0}, {1.5, 0}, 8.0},
-    {"128x128", 128, 128, 2, {0.45, 0.8}, {0.5, 0.9}, 4.0},
-    {"64x64", 64, 64, 2, {0.22, 0.4}, {0.22, 0.4}, 2.5},
+    {"256x256", 256, 256, 1, {{0.99, 1.59}, {kF8Never, kF8Never}, {2.49, 3.36}, {3.20, 3.90}}, {8.9, 9.0}},
+    {"256x128", 256, 128, 1, {{0.64, 0.88}, {0.84, 1.07}, {1.49, 1.74}, {1.75, 1.92}}, {5.1, 5.0}},
+    {"128x128", 128, 128, 2, {{0.58, 0.94}, {0.65, 1.06}, {1.04, 1.69}, {1.22, 1.87}}, {3.6, 3.3}},
+    {"64x64", 64, 64, 2, {{0.22, 0.36}, {0.27, 0.41}, {0.47, 0.63}, {0.53, 0.71}}, {2.8, 2.5}},
 };
 constexpr int kF8FormCount = sizeof(kF8Forms) / sizeof(kF8Forms[0]);
 constexpr uint32_t kF8Units = 256;
-constexpr double kF8Join = 4.5, kF8JoinBytes = 5e6;      // what joining parts of K costs besides; bytes a unit of cost
+constexpr double kF8Join = 3.0, kF8JoinSplit = 0.45, kF8JoinBytes = 10.5e6;      // what joining parts of K costs besides, for each part, bytes a unit of cost
 constexpr uint64_t kF8MostTiles = 1u << 22;              // of a launch
 
 inline uint32_t f8_steps(uint64_t k) { return uint32_t((k + 127) / 128); }
 
-inline double f8_cost(const F8Form &f, uint64_t m, uint64_t n, uint32_t steps, uint32_t splits, bool rows) {
+inline double f8_cost(const F8Form &f, uint64_t m, uint64_t n, uint32_t steps, uint32_t splits, bool wide, bool rows) {
     const uint64_t blocks = f.tiles(m, n) * splits, at_once = kF8Units * f.together, full = blocks / at_once, rest = blocks % at_once;
-    const double *step = rows ? f.step_rows : f.step;
-    double t = double(full) * (double(steps) * step[f.together - 1] + f.block);
-    if (rest) t += double(steps) * step[(rest + kF8Units - 1) / kF8Units - 1] + f.block;
+    const double *step = f.step[2 * wide + rows], block = f.block[wide || splits > 1];
+    double t = double(full) * (double(steps) * step[1] + block);
+    if (rest) t += double(steps) * step[rest > kF8Units] + block;
     return t;
 }
 
@@ -42,7 +47,7 @@ inline uint32_t f8_few_waves(uint64_t m, uint32_t steps) { return m > 16 ? 0 : s
 struct F8Choice { int form; uint32_t splits; };
 
 // The cheapest form and number of parts whose parts fit the workspace. Joining the parts costs another launch and the way of the parts to memory and back.
-inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool rows, uint64_t workspace) {
+inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool wide, bool rows, uint64_t workspace) {
     const uint32_t steps = f8_steps(k);
     F8Choice best{0, 1};
     double least = 0;
@@ -50,8 +55,8 @@ inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool rows, uint64_
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
             const uint32_t each = (steps + splits - 1) / splits;
             if (splits > 1 && (uint64_t(each) * (splits - 1) >= steps || f8_part_bytes(m, n) > workspace / splits || kF8Forms[f].tiles(m, n) > kF8MostTiles)) break;
-            double t = f8_cost(kF8Forms[f], m, n, each, splits, rows);
-            if (splits > 1) t += kF8Join + double(f8_part_bytes(m, n)) * (2 * splits + 1) / kF8JoinBytes;
+            double t = f8_cost(kF8Forms[f], m, n, each, splits, wide, rows);
+            if (splits > 1) t += kF8Join + kF8JoinSplit * splits + double(f8_part_bytes(m, n)) * (2 * splits + 1) / kF8JoinBytes;
             if ((f == 0 && splits == 1) || t < least) { best = F8Choice{f, splits}; least = t; }
         }
     return best;

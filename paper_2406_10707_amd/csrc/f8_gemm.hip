@@ -20,52 +20,80 @@ struct F8Gemm {
 
 // ------------------------------------------------------------------ tiles through LDS
 
-// Eight consecutive elements of a row of C, or the first `count` of them, at any element's address.
+// What a lane loads or stores of a row of C at once, at any element's address: sixteen bytes.
 template <int OUT>
-__device__ __forceinline__ void store_run(void *to, f32x4 lo, f32x4 hi, int64_t count, bool accumulate) {
-    typedef typename Element<OUT>::one One;
-    One *at = static_cast<One *>(to);
-    if (count >= 8) {
-        if (accumulate) {
-            lo += load4<OUT>(at);
-            hi += load4<OUT>(at + 4);
-        }
-        store8<OUT>(at, lo, hi);
-        return;
+struct Run {
+    static constexpr int COUNT = OUT == CKPT_F32 ? 4 : 8;
+    f32x4 v[COUNT / 4];
+    __device__ __forceinline__ void load(const void *at, int64_t count) {
+        typedef const typename Element<OUT>::one *Pointer;
+        if (count >= COUNT) {
+            if constexpr (OUT == CKPT_F32) v[0] = load4<OUT>(at);
+            else {
+                Eight<OUT> e;
+                e.load(at);
+                v[0] = __builtin_convertvector(e.lo, f32x4);
+                v[1] = __builtin_convertvector(e.hi, f32x4);
+            }
+        } else
+#pragma unroll
+            for (int h = 0; h < COUNT / 4; h++) v[h] = count > 4 * h ? load_upto4<OUT>((Pointer)at + 4 * h, uint32_t(count - 4 * h)) : f32x4{0, 0, 0, 0};
     }
-    if (count <= 0) return;
-    if (accumulate) {
-        lo += load_upto4<OUT>(at, uint32_t(count));
-        if (count > 4) hi += load_upto4<OUT>(at + 4, uint32_t(count - 4));
+    __device__ __forceinline__ void store(void *at, int64_t count) const {
+        typedef typename Element<OUT>::one *Pointer;
+        if (count >= COUNT) {
+            if constexpr (OUT == CKPT_F32) store4<OUT>(at, v[0]);
+            else store8<OUT>(at, v[0], v[1]);
+        } else
+#pragma unroll
+            for (int h = 0; h < COUNT / 4; h++)
+                if (count > 4 * h) store_upto4<OUT>((Pointer)at + 4 * h, v[h], uint32_t(count - 4 * h));
     }
-    store_upto4<OUT>(at, lo, uint32_t(count));
-    if (count > 4) store_upto4<OUT>(at + 4, hi, uint32_t(count - 4));
-}
+};
 
-// A wave's sums go to C through LDS, sixteen rows at a time (fragment i: rows ar TM + i), so that a store is runs of whole lines: a lane has 4 TNG columns of a row, neighbouring lanes other rows. Rows in LDS are 16 bytes longer than
-// their 16 TN sums: sixteen lanes' writes then go to different banks.
-template <class S, int OUT>
+// A wave's sums go to C through LDS, sixteen rows at a time (fragment i: rows ar TM + i), so that a store is whole lines: a lane has 4 TNG columns of a row, neighbouring lanes other rows. Rows in LDS are 16 bytes longer than their 16 TN
+// sums: sixteen lanes' writes then go to different banks.
+template <class S, int OUT, bool ADD>
 __device__ __forceinline__ void store_sums(const F8Gemm &p, f32x4 (&acc)[S::TM][S::TN], uint8_t *lds, int64_t row, int64_t col, int lane, int wave, int wm, int wn) {
     typedef typename Element<OUT>::one One;
-    constexpr int PITCH = 64 * S::TN + 16, LANES = 2 * S::TN, ROWS = 64 / LANES;      // lanes for a row's 16 TN columns
-    static_assert(S::NW * 16 * PITCH <= S::BYTES, "a wave's rows fit its part");
-    const int q = lane >> 4, ar = lane & 15, run = lane % LANES, in = lane / LANES;
+    typedef Run<OUT> Piece;
+    constexpr int PITCH = 64 * S::TN + 16, LANES = 16 * S::TN / Piece::COUNT, ROWS = 64 / LANES, TURNS = 16 / ROWS, BATCH = TURNS < 4 ? TURNS : 4;      // lanes for a row's 16 TN columns
+    static_assert(S::NW * 16 * PITCH <= S::BYTES && LANES <= 64 && TURNS % BATCH == 0, "a wave's rows fit its part");
+    const int q = lane >> 4, ar = lane & 15, piece = lane % LANES, in = lane / LANES;
     uint8_t *mine = lds + wave * 16 * PITCH;
-    const int64_t c_row = row + 16 * S::TM * wm, c_col = col + 16 * S::TN * wn + 8 * run, left = p.n - c_col;
+    const int64_t c_row = row + 16 * S::TM * wm, c_col = col + 16 * S::TN * wn + Piece::COUNT * piece, left = p.n - c_col;
     One *c = static_cast<One *>(p.c) + blockIdx.y * p.c_split + c_col;
+    const bool whole = row + S::BM <= p.m && col + S::BN <= p.n;
+    auto store = [&](auto whole_) {
 #pragma unroll
-    for (int i = 0; i < S::TM; i++) {
+        for (int i = 0; i < S::TM; i++) {
 #pragma unroll
-        for (int j = 0; j < S::TN; j++) *reinterpret_cast<f32x4 *>(mine + ar * PITCH + 4 * (16 * S::TNG * (j / S::TNG) + 4 * S::TNG * q + 4 * (j % S::TNG))) = acc[i][j];
-        asm volatile("" ::: "memory");      // other lanes' writes are read: a wave's go to LDS in the order of the program, which the compiler must not change
+            for (int j = 0; j < S::TN; j++) *reinterpret_cast<f32x4 *>(mine + ar * PITCH + 4 * (16 * S::TNG * (j / S::TNG) + 4 * S::TNG * q + 4 * (j % S::TNG))) = acc[i][j];
+            asm volatile("" ::: "memory");      // other lanes' writes are read: a wave's go to LDS in the order of the program, which the compiler must not change
 #pragma unroll
-        for (int t = 0; t < 16; t += ROWS) {
-            const int64_t r = c_row + S::TM * (t + in) + i;
-            const f32x4 *at = reinterpret_cast<const f32x4 *>(mine + (t + in) * PITCH + 32 * run);
-            if (r < p.m) store_run<OUT>(c + r * p.ldc, at[0], at[1], left, p.accumulate);
+            for (int t0 = 0; t0 < TURNS; t0 += BATCH) {
+                Piece old[BATCH];
+#pragma unroll
+                for (int t = 0; t < BATCH; t++) {
+                    const int64_t r = c_row + S::TM * (ROWS * (t0 + t) + in) + i;
+                    if constexpr (ADD)
+                        if (whole_ || r < p.m) old[t].load(c + r * p.ldc, whole_ ? Piece::COUNT : left);
+                }
+#pragma unroll
+                for (int t = 0; t < BATCH; t++) {
+                    const int64_t r = c_row + S::TM * (ROWS * (t0 + t) + in) + i;
+                    const f32x4 *at = reinterpret_cast<const f32x4 *>(mine + (ROWS * (t0 + t) + in) * PITCH + 4 * Piece::COUNT * piece);
+                    Piece out;
+#pragma unroll
+                    for (int h = 0; h < Piece::COUNT / 4; h++) out.v[h] = ADD ? at[h] + old[t].v[h] : at[h];
+                    if (whole_ || (r < p.m && left > 0)) out.store(c + r * p.ldc, whole_ ? Piece::COUNT : left);
+                }
+            }
+            asm volatile("" ::: "memory");
         }
-        asm volatile("" ::: "memory");
-    }
+    };
+    if (whole) store(std::true_type{});
+    else store(std::false_type{});
 }
 
 template <class S, bool SQUARE, bool WIDE, int FA, int FB>
@@ -78,9 +106,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void f8_gemm_kernel(F8Gemm p, TileOr
     const F8Loader<S> load(p.a, p.b, p.b, p.steps, row, col, lane, wave);
     f32x4 acc[S::TM][S::TN];
     f8_sums<S, SQUARE, WIDE, FA, FB>(acc, lds, load, first, min(p.steps - first, p.steps_a_split), lane, wm, wn);
-    if (p.dtype == CKPT_F32) store_sums<S, CKPT_F32>(p, acc, lds, row, col, lane, wave, wm, wn);
-    else if (p.dtype == CKPT_BF16) store_sums<S, CKPT_BF16>(p, acc, lds, row, col, lane, wave, wm, wn);
-    else store_sums<S, CKPT_F16>(p, acc, lds, row, col, lane, wave, wm, wn);
+    auto out = [&](auto dtype) {
+        if (p.accumulate) store_sums<S, dtype, true>(p, acc, lds, row, col, lane, wave, wm, wn);
+        else store_sums<S, dtype, false>(p, acc, lds, row, col, lane, wave, wm, wn);
+    };
+    if (p.dtype == CKPT_F32) out(std::integral_constant<int, CKPT_F32>());
+    else if constexpr (!WIDE) {
+        if (p.dtype == CKPT_BF16) out(std::integral_constant<int, CKPT_BF16>());
+        else out(std::integral_constant<int, CKPT_F16>());
+    }
 }
 
 // ------------------------------------------------------------------ up to sixteen rows of A
@@ -163,13 +197,16 @@ void launch_form(const F8Choice &choice, const F8Gemm &p, bool wide, bool a_e5m2
                 typedef decltype(shape) S;
                 const dim3 grid(tiles_m * tiles_n, choice.splits), block(S::THREADS);
                 const TileOrder order(tiles_m, tiles_n, true);
-                auto launch = [&](auto square, auto wide_) { hipLaunchKernelGGL((f8_gemm_kernel<S, square, wide_, fa, fb>), grid, block, 0, stream, part, order); };
+                auto launch = [&](auto square, auto wide_) {
+                    if constexpr (square || wide_ || S::BN < 256) hipLaunchKernelGGL((f8_gemm_kernel<S, square, wide_, fa, fb>), grid, block, 0, stream, part, order);      // kF8Never
+                };
                 if (part.b.shift) wide ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
                 else wide ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
             };
             switch (choice.form) {
                 case 0: go(F8Shape<4, 2, 4, 8, 4, 2, false>()); break;
-                case 1: go(F8Shape<2, 2, 4, 4, 4, 2, false>()); break;
+                case 1: go(F8Shape<4, 2, 4, 4, 4, 3, false>()); break;
+                case 2: go(F8Shape<2, 2, 4, 4, 4, 2, false>()); break;
                 default: go(F8Shape<2, 2, 2, 2, 2, 4, false>()); break;
             }
         });
@@ -206,7 +243,7 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
         });
         return launched();
     }
-    const F8Choice choice = f8_choice(uint64_t(m), uint64_t(n), uint64_t(k), !p.b.shift, workspace ? workspace_bytes : 0);
+    const F8Choice choice = f8_choice(uint64_t(m), uint64_t(n), uint64_t(k), wide, !p.b.shift, workspace ? workspace_bytes : 0);
     if (choice.splits == 1) {
         launch_form(choice, p, wide, a_e5m2, b_e5m2, stream);
         return launched();
@@ -237,8 +274,8 @@ int ckpt_f8_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes) {
         *bytes = 0;
         if (m > 0x7FFFFFFF || n > 0x7FFFFFFF || k > kF8LongestRow) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1, or what is contracted over 2^23");
         if (!m || !n || !k || f8_few_waves(uint64_t(m), f8_steps(uint64_t(k)))) return int(CKPT_OK);
-        for (bool rows : {false, true}) {
-            const F8Choice c = f8_choice(uint64_t(m), uint64_t(n), uint64_t(k), rows, UINT64_MAX);
+        for (int kind = 0; kind < 4; kind++) {
+            const F8Choice c = f8_choice(uint64_t(m), uint64_t(n), uint64_t(k), kind & 1, kind >> 1, UINT64_MAX);
             if (c.splits > 1) *bytes = std::max(*bytes, f8_part_bytes(uint64_t(m), uint64_t(n)) * c.splits);
         }
         return int(CKPT_OK);

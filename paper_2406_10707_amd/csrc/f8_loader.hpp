@@ -31,36 +31,45 @@ struct F8Shape {
 
 __device__ __forceinline__ uint32_t f8_rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
 
+// Rows past the end of a matrix lie past the descriptor's end, so that they are not read; what LDS has in their places counts for nothing that is stored. (The scalar offset, the step's, counts or does not count in that check: a row inside is inside
+// either way, the next row's first byte is outside.) Their scales are the last row's.
 template <class S>
 struct F8Loader {
-    __amdgpu_buffer_rsrc_t ra, rb[S::LB];
-    uint32_t off[S::LA + S::LB], wave;
+    __amdgpu_buffer_rsrc_t ra, rb[2];
+    uint32_t pitch_a, pitch_b[2], row_a, row_b, piece, wave;      // this lane's rows with the wave's first load, and what part of a row
     const float *scale;
     uint64_t scale_pitch;
 
+    static constexpr uint32_t row_of_place_a(uint32_t place) { return place / (16 * S::TM) * (16 * S::TM) + S::TM * (place % 16) + place / 16 % S::TM; }
+    static constexpr uint32_t row_of_place_b(uint32_t place) { return place / (16 * S::TNG) * (16 * S::TNG) + 4 * S::TNG * (place % 16 / 4) + 4 * (place / 16 % S::TNG) + place % 4; }
     // which of the two matrices, and which row behind the tile's first, the tile's row n of B is
-    static __device__ __forceinline__ uint32_t matrix_of(uint32_t n) { return S::PAIR ? (n / (16 * S::TNG)) & 1 : 0; }
-    static __device__ __forceinline__ uint32_t row_of(uint32_t n) { return S::PAIR ? n / (32 * S::TNG) * (16 * S::TNG) + n % (16 * S::TNG) : n; }
+    static constexpr uint32_t matrix_of(uint32_t n) { return S::PAIR ? n / (16 * S::TNG) & 1 : 0; }
+    static constexpr uint32_t row_of(uint32_t n) { return S::PAIR ? n / (32 * S::TNG) * (16 * S::TNG) + n % (16 * S::TNG) : n; }
 
     __device__ __forceinline__ F8Loader(const F8Side a, const F8Side b, const F8Side b2, uint32_t steps, int64_t row, int64_t col, int lane, uint32_t wave_) : wave(wave_) {
         constexpr int ROWS_B = S::PAIR ? S::BN / 2 : S::BN;
-        const uint32_t last_a = uint32_t(min(a.rows - row, int64_t(S::BM)) - 1), last_b = uint32_t(min(b.rows - col, int64_t(ROWS_B)) - 1);      // rows past the end are the last row again
-        const uint32_t in_8 = lane >> 3, piece = 16 * ((lane & 7) ^ f8_rotated(((lane >> 4) & 3) | ((wave & 1) << 2)));
-        ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes + row * a.pitch), 0, last_a * uint32_t(a.pitch) + 128 * steps, 0x00020000);
-#pragma unroll
-        for (int c = 0; c < S::LA; c++) {
-            const uint32_t place = 8 * (S::NW * c + wave) + in_8, r = place / (16 * S::TM) * (16 * S::TM) + S::TM * (place % 16) + place / 16 % S::TM;
-            off[c] = min(r, last_a) * uint32_t(a.pitch) + piece;
-        }
-#pragma unroll
-        for (int c = 0; c < S::LB; c++) {
-            const uint32_t first = 8 * (S::NW * c + wave), place = first + in_8, ar = place % 16;
-            const uint32_t n = place / (16 * S::TNG) * (16 * S::TNG) + 4 * S::TNG * (ar / 4) + 4 * (place / 16 % S::TNG) + ar % 4;
-            const uint8_t *base = b.codes;
-            uint64_t pitch = b.pitch;
-            if (S::PAIR && matrix_of(first)) { base = b2.codes; pitch = b2.pitch; }
-            off[S::LA + c] = min(row_of(n), last_b) * uint32_t(pitch) + piece;
-            rb[c] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base + col * pitch), 0, last_b * uint32_t(pitch) + 128 * steps, 0x00020000);
+        const uint32_t last_a = uint32_t(min(a.rows - row, int64_t(S::BM)) - 1), last_b = uint32_t(min(b.rows - col, int64_t(ROWS_B)) - 1);
+        // a load's places are those of the first load and a multiple of 8 NW: sizes are powers of two, so that its rows are the sum of both places' rows
+        const uint32_t place = 8 * wave + (lane >> 3);
+        row_a = row_of_place_a(place);
+        row_b = row_of(row_of_place_b(place));
+        piece = 16 * ((lane & 7) ^ f8_rotated(((lane >> 4) & 3) | ((wave & 1) << 2)));
+        auto descriptor = [&](const F8Side &side, int64_t first, uint32_t last) {
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(side.codes + first * side.pitch), 0, last * uint32_t(side.pitch) + 128 * steps, 0x00020000);
+        };
+        ra = descriptor(a, row, last_a);
+        rb[0] = descriptor(b, col, last_b);
+        rb[1] = S::PAIR ? descriptor(b2, col, last_b) : rb[0];
+        pitch_a = uint32_t(a.pitch);
+        pitch_b[0] = uint32_t(b.pitch);
+        pitch_b[1] = uint32_t(b2.pitch);
+        if (S::PAIR && matrix_of(8 * wave)) {      // this wave's loads begin with the second
+            const auto r = rb[0];
+            rb[0] = rb[1];
+            rb[1] = r;
+            const uint32_t p = pitch_b[0];
+            pitch_b[0] = pitch_b[1];
+            pitch_b[1] = p;
         }
         const uint32_t slot = 64 * wave;      // of the wave's first lane: a wave's scales are all A's or all B's
         if (slot < S::BM) {
@@ -77,13 +86,16 @@ struct F8Loader {
     // all loads of a step into a stage
     __device__ __forceinline__ void issue(uint8_t *stage, uint32_t step) const {
 #pragma unroll
-        for (int c = 0; c < S::LA + S::LB; c++) issue(stage, step, c);
-        issue(stage, step, S::LA + S::LB);
+        for (int c = 0; c < S::LOADS; c++) issue(stage, step, c);
     }
     __device__ __forceinline__ void issue(uint8_t *stage, uint32_t step, int c) const {
-        if (c < S::LA) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (DSLLM_LDS void *)(stage + 1024 * (S::NW * c + wave)), 16, off[c], 128 * step, 0, 0);
-        else if (c < S::LA + S::LB) __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[c < S::LA ? 0 : c - S::LA], (DSLLM_LDS void *)(stage + S::BM * 128 + 1024 * (S::NW * (c - S::LA) + wave)), 16, off[c], 128 * step, 0, 0);
-        else __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(scale + step * scale_pitch), (DSLLM_LDS void *)(stage + S::CODES + 256 * wave), 4, 0, 0);
+        if (c < S::LA) {
+            const uint32_t at = (row_a + row_of_place_a(8 * S::NW * c)) * pitch_a + piece;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (DSLLM_LDS void *)(stage + 1024 * (S::NW * c + wave)), 16, at, 128 * step, 0, 0);
+        } else if (c < S::LA + S::LB) {
+            const uint32_t first = 8 * S::NW * (c - S::LA), which = matrix_of(first), at = (row_b + row_of(row_of_place_b(first))) * pitch_b[which] + piece;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[which], (DSLLM_LDS void *)(stage + S::BM * 128 + 1024 * (S::NW * (c - S::LA) + wave)), 16, at, 128 * step, 0, 0);
+        } else __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(scale + step * scale_pitch), (DSLLM_LDS void *)(stage + S::CODES + 256 * wave), 4, 0, 0);
     }
 };
 

@@ -50,79 +50,240 @@ __device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t hi) {
     }
     return __builtin_bit_cast(bf16x8, r);
 }
-// What a fragment is to the matrix instructions: a lane's 32 codes of a step, or those as bf16. Any order of K will do that both sides share.
-template <bool WIDE, int FORMAT> struct F8Fragment {
-    i32x8 codes;
-    __device__ __forceinline__ void set(u32x4 lo, u32x4 hi) { codes = i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; }
-};
-template <int FORMAT> struct F8Fragment<true, FORMAT> {
-    bf16x8 eights[4];
-    __device__ __forceinline__ void set(u32x4 lo, u32x4 hi) {
-        eights[0] = widened<FORMAT>(lo.x, lo.y);
-        eights[1] = widened<FORMAT>(lo.z, lo.w);
-        eights[2] = widened<FORMAT>(hi.x, hi.y);
-        eights[3] = widened<FORMAT>(hi.z, hi.w);
+// The sums over steps [first, first + steps) of K. SQUARE: B's scales are those of 128 x 128, one for a group of columns. acc[i][j][e]: row 16 TM wm + TM ar + i, column 16 TN wn + 16 TNG (j / TNG) + 4 TNG q + 4 (j mod TNG) + e.
+//
+// The wave's own order is fixed by hand, and two waves share a SIMD. A's fragments of a step stay in registers, B's come one after the other; beside the matrix instructions stand the reads and conversions of what later ones need, and the
+// multiply-adds of the sums that were in the place of theirs. One barrier a step, before its last fragments: then every wave has read the whole stage, and all loads of the next have landed, which were issued a step (STAGES - 1 steps)
+// before. Behind it come the loads into the stage that is free now, and the reads of the next: A's fragments take the places of those whose last matrix instruction has been issued.
+template <class S, bool SQUARE>
+struct F8Stages {
+    static constexpr int TM = S::TM, TN = S::TN, TNG = S::TNG;
+    const F8Loader<S> &load;
+    uint8_t *lds;
+    const uint8_t *from;      // the stage that is read
+    uint32_t first, steps, next, into;      // the stage behind it; the one that loads go to
+    int x[2], base_a, base_b, scales_a, scales_b;      // a lane's two pieces of a place; places of the wave
+    float sa[TM], sb[TN / TNG];
+
+    // AHEAD: loads of a step that are out when the step before the STAGES - 1 before begins
+    __device__ __forceinline__ F8Stages(uint8_t *lds_, const F8Loader<S> &load_, uint32_t first_, uint32_t steps_, int lane, int wm, int wn, int ahead)
+        : load(load_), lds(lds_), from(lds_), first(first_), steps(steps_), next(S::STAGE), into((S::STAGES - 1) * S::STAGE) {
+        const int q = lane >> 4, ar = lane & 15, swizzle = f8_rotated((ar >> 1) & 7);
+        x[0] = ar * 128 + 16 * ((2 * q) ^ swizzle);
+        x[1] = ar * 128 + 16 * ((2 * q + 1) ^ swizzle);
+        base_a = wm * TM * 2048;
+        base_b = S::BM * 128 + wn * TN * 2048;
+        scales_a = S::CODES + 4 * (16 * TM * wm + TM * ar);
+        scales_b = S::CODES + 4 * (S::BM + 16 * TN * wn) + (SQUARE ? 0 : 16 * TNG * q);
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; s++) load.issue(lds + s * S::STAGE, first + min(uint32_t(s), steps - 1));
+#pragma unroll
+        for (int c = 0; c < ahead; c++) load.issue(lds + into, first + min(uint32_t(S::STAGES - 1), steps - 1), c);
     }
+    // load c of the step `behind` the current one; past the end the last step's again, into a stage that nothing reads
+    __device__ __forceinline__ void issue(uint32_t s, int behind, int c) const { load.issue(lds + into, first + min(s + behind, steps - 1), c); }
+    __device__ __forceinline__ void turn() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S::STAGES - 2) * S::LOADS) : "memory");
+        from = lds + next;
+        next = next + S::STAGE == S::BYTES ? 0 : next + S::STAGE;
+        into = into + S::STAGE == S::BYTES ? 0 : into + S::STAGE;
+    }
+    __device__ __forceinline__ u32x2 quarter(int base, int k) const { return *reinterpret_cast<const u32x2 *>(from + base + x[k >> 1] + 8 * (k & 1)); }
+    __device__ __forceinline__ u32x4 half(int base, int h) const { return *reinterpret_cast<const u32x4 *>(from + base + x[h]); }
+    __device__ __forceinline__ i32x8 fragment(int base) const {
+        const u32x4 lo = half(base, 0), hi = half(base, 1);
+        return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+    }
+    __device__ __forceinline__ int a_at(int i) const { return base_a + 2048 * i; }
+    __device__ __forceinline__ int b_at(int j) const { return base_b + 2048 * j; }
+    __device__ __forceinline__ void read_scales() {
+#pragma unroll
+        for (int i = 0; i < TM; i++) sa[i] = *reinterpret_cast<const float *>(from + scales_a + 4 * i);
+        if constexpr (SQUARE)
+#pragma unroll
+            for (int g = 0; g < TN / TNG; g++) sb[g] = *reinterpret_cast<const float *>(from + scales_b + 64 * TNG * g);
+    }
+    __device__ __forceinline__ f32x4 row_scales(int j) const { return *reinterpret_cast<const f32x4 *>(from + scales_b + 4 * (16 * TNG * (j / TNG) + 4 * (j % TNG))); }
 };
 
-// The sums over steps [first, first + steps) of K. SQUARE: B's scales are those of 128 x 128, one for a group of columns. acc[i][j][e]: row 16 TM wm + TM ar + i, column 16 TN wn + 16 TNG (j / TNG) + 4 TNG q + 4 (j mod TNG) + e.
-template <class S, bool SQUARE, bool WIDE, int FA, int FB>
-__device__ __forceinline__ void f8_sums(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds, const F8Loader<S> &load, uint32_t first, uint32_t steps, int lane, int wm, int wn) {
-    const int q = lane >> 4, ar = lane & 15;
+template <class S>
+__device__ __forceinline__ void f8_clear(f32x4 (&acc)[S::TM][S::TN]) {
 #pragma unroll
     for (int i = 0; i < S::TM; i++)
 #pragma unroll
         for (int j = 0; j < S::TN; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+}
+
+// In bf16: a step is TN times 4 blocks of TM matrix instructions, a quarter of fragment j (8 of a lane's 32 codes; any order of K will do that both sides share) with those of all of A's fragments. A block's next quarter of B is converted in
+// front of it; those of A's next fragments in the blocks behind the barrier.
+template <class S, bool SQUARE, int FA, int FB>
+__device__ __forceinline__ void f8_sums_wide(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds, const F8Loader<S> &load, uint32_t first, uint32_t steps, int lane, int wm, int wn) {
+    constexpr int TM = S::TM, TN = S::TN, BLOCKS = 4 * TN, LAST = BLOCKS - 4, A_BLOCK = (S::LOADS + BLOCKS - 1) / BLOCKS, AHEAD = 4 * A_BLOCK < S::LOADS ? 4 * A_BLOCK : S::LOADS;
+    static_assert(TN % 2 == 0 && BLOCKS * A_BLOCK >= S::LOADS, "a step's loads are out within a step");
+    f8_clear<S>(acc);
     if (!steps) return;
+    F8Stages<S, SQUARE> in(lds, load, first, steps, lane, wm, wn, AHEAD);
+    bf16x8 a[TM][4], b[2];      // b: the quarter that counts and the next
+    u32x2 raw_a[TM];            // a quarter that is still to be converted
+    u32x4 raw_b[2];
+    f32x4 sum[TM], sb_rows[2];
+    float scale[TM], sa_before[TM];
+    auto add = [&](int i, int j) {
 #pragma unroll
-    for (int s = 0; s < S::STAGES; s++) load.issue(lds + s * S::STAGE, first + min(uint32_t(s), steps - 1));
-    const int swizzle = f8_rotated((ar >> 1) & 7), x0 = ar * 128 + 16 * ((2 * q) ^ swizzle), x1 = ar * 128 + 16 * ((2 * q + 1) ^ swizzle);
-    const int base_a = wm * S::TM * 2048, base_b = S::BM * 128 + wn * S::TN * 2048;
-    const int scales_a = S::CODES + 4 * (16 * S::TM * wm + S::TM * ar), scales_b = S::CODES + 4 * (S::BM + 16 * S::TN * wn);
-    uint32_t at = 0;      // the stage's place
-    for (uint32_t s = 0; s < steps; s++) {
-        uint8_t *stage = lds + at;
-        at = at + S::STAGE == S::BYTES ? 0 : at + S::STAGE;
-        wait_loads_and_meet<(S::STAGES - 1) * S::LOADS>();
-        auto read = [&](auto &f, int base) { f.set(*reinterpret_cast<const u32x4 *>(stage + base + x0), *reinterpret_cast<const u32x4 *>(stage + base + x1)); };
-        float sa[S::TM];
+        for (int e = 0; e < 4; e++)
+            if constexpr (SQUARE) acc[i][j][e] = __builtin_fmaf(sum[i][e], scale[i], acc[i][j][e]);
+            else acc[i][j][e] = __builtin_fmaf(sum[i][e], (j == TN - 1 ? sa_before[i] : in.sa[i]) * sb_rows[j & 1][e], acc[i][j][e]);
+    };
+    wait_loads_and_meet<(S::STAGES - 2) * S::LOADS + AHEAD>();
+    in.read_scales();
 #pragma unroll
-        for (int i = 0; i < S::TM; i++) sa[i] = *reinterpret_cast<const float *>(stage + scales_a + 4 * i);
-        F8Fragment<WIDE, FA> fa[S::TM];
+    for (int i = 0; i < TM; i++) {
+        sum[i] = f32x4{0, 0, 0, 0};      // in the place of the fragment before the first: adds nothing
+        scale[i] = sa_before[i] = 0;
 #pragma unroll
-        for (int i = 0; i < S::TM; i++) read(fa[i], base_a + 2048 * i);
-#pragma unroll
-        for (int j = 0; j < S::TN; j++) {
-            F8Fragment<WIDE, FB> fb;
-            read(fb, base_b + 2048 * j);
-            const uint8_t *sb_at = stage + scales_b + 4 * (16 * S::TNG * (j / S::TNG) + (SQUARE ? 0 : 4 * S::TNG * q + 4 * (j % S::TNG)));
-            f32x4 sum[S::TM];
-            if constexpr (WIDE) {
-#pragma unroll
-                for (int k = 0; k < 4; k++)
-#pragma unroll
-                    for (int i = 0; i < S::TM; i++) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb.eights[k], fa[i].eights[k], k ? sum[i] : f32x4{0, 0, 0, 0}, 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int i = 0; i < S::TM; i++) sum[i] = mfma_f8<FA, FB>(fb.codes, fa[i].codes);
-            }
-#pragma unroll
-            for (int i = 0; i < S::TM; i++) {
-                if constexpr (SQUARE) {
-                    const float scale = sa[i] * *reinterpret_cast<const float *>(sb_at);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(sum[i][e], scale, acc[i][j][e]);
-                } else {
-                    const f32x4 sb = *reinterpret_cast<const f32x4 *>(sb_at);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(sum[i][e], sa[i] * sb[e], acc[i][j][e]);
-                }
-            }
+        for (int k = 0; k < 3; k++) {
+            const u32x2 r = in.quarter(in.a_at(i), k);
+            a[i][k] = widened<FA>(r.x, r.y);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // no wave reads this stage any more
-        load.issue(stage, first + min(s + S::STAGES, steps - 1));
+        raw_a[i] = in.quarter(in.a_at(i), 3);
     }
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");      // no load to LDS is under way
+#pragma unroll
+    for (int h = 0; h < 2; h++) raw_b[h] = in.half(in.b_at(0), h);
+    b[0] = widened<FB>(raw_b[0].x, raw_b[0].y);
+    sb_rows[1] = f32x4{0, 0, 0, 0};
+    if constexpr (!SQUARE) sb_rows[0] = in.row_scales(0);
+    __builtin_amdgcn_sched_barrier(0);
+    for (uint32_t s = 0; s < steps; s++)
+        for_each_of([&](auto index) {
+            constexpr int at = index, j = at / 4, k = at % 4, before = (j + TN - 1) % TN, to_j = (j + 1) % TN, to_k = (k + 1) % 4;
+            if constexpr (at == LAST) in.turn();
+#pragma unroll
+            for (int i = 0; i < TM; i++) {
+                if constexpr (k == 0) add(i, before);
+                sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[at & 1], a[i][k], k ? sum[i] : f32x4{0, 0, 0, 0}, 0, 0, 0);
+            }
+            if constexpr (k == 0 && SQUARE && j % S::TNG == 0)
+#pragma unroll
+                for (int i = 0; i < TM; i++) scale[i] = in.sa[i] * in.sb[j / S::TNG];
+            b[(at & 1) ^ 1] = widened<FB>(raw_b[to_k / 2][to_k % 2 * 2], raw_b[to_k / 2][to_k % 2 * 2 + 1]);
+            if constexpr (k % 2 == 0) raw_b[k / 2] = in.half(in.b_at(to_j), k / 2);      // both its quarters are converted
+            if constexpr (at > LAST || at == 0)
+#pragma unroll
+                for (int i = 0; i < TM; i++) a[i][(k + 3) % 4] = widened<FA>(raw_a[i].x, raw_a[i].y);
+            if constexpr (at >= LAST)
+#pragma unroll
+                for (int i = 0; i < TM; i++) raw_a[i] = in.quarter(in.a_at(i), k);
+            if constexpr (!SQUARE && k == 3 && at < LAST) sb_rows[(j + 1) & 1] = in.row_scales(j + 1);      // in the place of those that have been used
+            if constexpr (at == BLOCKS - 1) {
+                if constexpr (!SQUARE) {
+#pragma unroll
+                    for (int i = 0; i < TM; i++) sa_before[i] = in.sa[i];
+                    sb_rows[0] = in.row_scales(0);
+                }
+                in.read_scales();
+            }
+            // a step's loads begin in the block of the barrier and go on in the next step
+            constexpr int turn = (at + BLOCKS - LAST) % BLOCKS;
+#pragma unroll
+            for (int c = turn * A_BLOCK; c < (turn + 1) * A_BLOCK && c < S::LOADS; c++) in.issue(s, at >= LAST ? S::STAGES : S::STAGES - 1, c);
+            __builtin_amdgcn_sched_barrier(0);
+        }, std::make_integer_sequence<int, BLOCKS>{});
+#pragma unroll
+    for (int i = 0; i < TM; i++) add(i, TN - 1);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // no load to LDS is under way
+}
+
+// In 8 bits: one matrix instruction for a fragment of A with one of B. A step takes B's fragments one after the other up to the last two, then A's with both of these: so each of A's is free soon, and the reads of the next, of all waves behind
+// the barrier, are spread over two fragments' time (with one, 8192^3 took 512 us).
+template <class S, bool SQUARE, int FA, int FB>
+__device__ __forceinline__ void f8_sums_narrow(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds, const F8Loader<S> &load, uint32_t first, uint32_t steps, int lane, int wm, int wn) {
+    constexpr int TM = S::TM, TN = S::TN, COUNT = TM * TN, LAST = COUNT - 2 * TM, EVERY = COUNT / S::LOADS > 0 ? COUNT / S::LOADS : 1, AT_ONCE = (S::LOADS * EVERY + COUNT - 1) / COUNT;
+    static_assert(TN % 2 == 0 && TN <= 8, "");
+    // load c goes out behind matrix instruction LAST + c / AT_ONCE * EVERY, of the step or of the next
+    constexpr int AHEAD = ((COUNT - LAST + EVERY - 1) / EVERY) * AT_ONCE < S::LOADS ? ((COUNT - LAST + EVERY - 1) / EVERY) * AT_ONCE : S::LOADS;
+    static_assert((S::LOADS + AT_ONCE - 1) / AT_ONCE * EVERY <= COUNT, "a step's loads are out within a step");
+    constexpr int PLACES = TN > 2 ? 4 : 2;      // of B's fragments
+    f8_clear<S>(acc);
+    if (!steps) return;
+    F8Stages<S, SQUARE> in(lds, load, first, steps, lane, wm, wn, AHEAD);
+    i32x8 a[TM], b[PLACES];
+    f32x4 sum[TM], sb_rows[SQUARE ? 1 : TN];
+    float scale[TN / S::TNG][TM];      // of the step before until they have been used
+    wait_loads_and_meet<(S::STAGES - 2) * S::LOADS + AHEAD>();
+    // which fragments instruction n of a step takes
+    auto row_of = [](int n) constexpr { return n < LAST ? n % TM : (n - LAST) / 2; };
+    auto col_of = [](int n) constexpr { return n < LAST ? n / TM : TN - 2 + (n - LAST) % 2; };
+    float sa_before[TM];
+    f32x4 sb_before[2];
+    auto add = [&](int n, bool of_step_before) {
+        const int i = row_of(n), j = col_of(n);
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if constexpr (SQUARE) acc[i][j][e] = __builtin_fmaf(sum[n % TM][e], scale[j / S::TNG][i], acc[i][j][e]);
+            else acc[i][j][e] = __builtin_fmaf(sum[n % TM][e], of_step_before ? sa_before[i] * sb_before[j % 2][e] : in.sa[i] * sb_rows[j][e], acc[i][j][e]);
+    };
+    in.read_scales();
+    if constexpr (!SQUARE)
+#pragma unroll
+        for (int j = 0; j < TN; j++) sb_rows[j] = in.row_scales(j);
+    sb_before[0] = sb_before[1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < TM; i++) {
+        sum[i] = f32x4{0, 0, 0, 0};
+        sa_before[i] = 0;
+#pragma unroll
+        for (int g = 0; g < TN / S::TNG; g++) scale[g][i] = 0;
+        a[i] = in.fragment(in.a_at(i));
+    }
+    b[0] = in.fragment(in.b_at(0));
+    b[1] = in.fragment(in.b_at(1));
+    __builtin_amdgcn_sched_barrier(0);
+    for (uint32_t s = 0; s < steps; s++)
+        for_each_of([&](auto index) {
+            constexpr int n = index, i = row_of(n), j = col_of(n);
+            if constexpr (n == LAST) in.turn();
+            add((n + COUNT - TM) % COUNT, n < TM);
+            sum[n % TM] = mfma_f8<FA, FB>(b[j % PLACES], a[i]);
+            // the scales of a group of columns, once the step before needs them no more: the last group's behind its last sums
+            if constexpr (SQUARE && n == TM - 1)
+#pragma unroll
+                for (int g = 0; g < TN / S::TNG; g++)
+#pragma unroll
+                    for (int r = 0; r < TM; r++) scale[g][r] = in.sa[r] * in.sb[g];
+            if constexpr (n < LAST && n % TM == 0 && j + 2 < TN) b[(j + 2) % PLACES] = in.fragment(in.b_at(j + 2));
+            if constexpr (n >= LAST && n % 2 == 1) a[i] = in.fragment(in.a_at(i));
+            if constexpr (PLACES == 4 && n == LAST) b[0] = in.fragment(in.b_at(0));
+            if constexpr (PLACES == 4 && n == LAST + TM) b[1] = in.fragment(in.b_at(1));
+            if constexpr (n == COUNT - 1) {
+                if constexpr (PLACES == 2) {
+                    b[0] = in.fragment(in.b_at(0));
+                    b[1] = in.fragment(in.b_at(1));
+                }
+                if constexpr (!SQUARE) {
+#pragma unroll
+                    for (int r = 0; r < TM; r++) sa_before[r] = in.sa[r];
+                    sb_before[0] = sb_rows[TN - 2];
+                    sb_before[1] = sb_rows[TN - 1];
+#pragma unroll
+                    for (int c = 0; c < TN; c++) sb_rows[c] = in.row_scales(c);
+                }
+                in.read_scales();
+            }
+            constexpr int turn = (n + COUNT - LAST) % COUNT;
+            if constexpr (turn % EVERY == 0)
+#pragma unroll
+                for (int c = turn / EVERY * AT_ONCE; c < (turn / EVERY + 1) * AT_ONCE && c < S::LOADS; c++) in.issue(s, n >= LAST ? S::STAGES : S::STAGES - 1, c);
+            if constexpr (n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        }, std::make_integer_sequence<int, COUNT>{});
+#pragma unroll
+    for (int n = COUNT - TM; n < COUNT; n++) add(n, true);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+template <class S, bool SQUARE, bool WIDE, int FA, int FB>
+__device__ __forceinline__ void f8_sums(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds, const F8Loader<S> &load, uint32_t first, uint32_t steps, int lane, int wm, int wn) {
+    if constexpr (WIDE) f8_sums_wide<S, SQUARE, FA, FB>(acc, lds, load, first, steps, lane, wm, wn);
+    else f8_sums_narrow<S, SQUARE, FA, FB>(acc, lds, load, first, steps, lane, wm, wn);
 }
 
 // ------------------------------------------------------------------ up to sixteen rows of A
@@ -168,15 +329,14 @@ struct F8Few {
                     load.issue_step(mine, window + WAVES, s);
                 }
                 if (4 * window + s >= steps) continue;
-                F8Fragment<true, FA> fa;
-                fa.set(lo[0], hi[0]);
+                const bf16x8 fa[4] = {widened<FA>(lo[0].x, lo[0].y), widened<FA>(lo[0].z, lo[0].w), widened<FA>(hi[0].x, hi[0].y), widened<FA>(hi[0].z, hi[0].w)};
 #pragma unroll
                 for (int x = 0; x < MATRICES; x++) {
-                    F8Fragment<true, FB> fb;
-                    fb.set(lo[1 + x], hi[1 + x]);
+                    const u32x4 l = lo[1 + x], h = hi[1 + x];
+                    const bf16x8 fb[4] = {widened<FB>(l.x, l.y), widened<FB>(l.z, l.w), widened<FB>(h.x, h.y), widened<FB>(h.z, h.w)};
                     f32x4 block{0, 0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < 4; k++) block = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb.eights[k], fa.eights[k], block, 0, 0, 0);
+                    for (int k = 0; k < 4; k++) block = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[k], fa[k], block, 0, 0, 0);
 #pragma unroll
                     for (int e = 0; e < 4; e++) sum[x][e] = __builtin_fmaf(block[e], sa * sb[x][e], sum[x][e]);
                 }
