@@ -136,20 +136,20 @@ int ckpt_f8_gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int3
  *   CKPT_GATE_GELU  act(g) = g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
 typedef enum { CKPT_GATE_SILU = 1, CKPT_GATE_GELU = 2 } ckpt_gate;
 
-/* Both projections, the activation, the product and the rounding to 8 bits in one pass. x is tokens x hidden, w_gate and w_up are ffn x hidden (one format,
+/* Both projections, the activation, the product and the rounding to 8 bits in one pass. x is tokens x hidden, w_gate and w_up are ffn x hidden (CKPT_F8_E4M3,
  * blocks of one kind); gate, up and h are tokens x ffn, CKPT_F8_E4M3 with block_rows 1. gate and up are what the backward pass needs, rounded to 8
  * bits (h is made of the values before that rounding); both NULL: nothing is kept, as in serving. Workspace as in ckpt_f8_gemm, for few tokens. */
 int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *bytes);
 int ckpt_gated_forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8_matrix *w_up, int32_t activation, const ckpt_f8_matrix *gate,
                        const ckpt_f8_matrix *up, const ckpt_f8_matrix *h, void *workspace, uint64_t workspace_bytes, void *stream);
 
-/* What ckpt_gated_backward writes, each or NULL, all with block_rows 1, gradients in either format, h as CKPT_F8_E4M3: by rows (tokens x ffn) for dx = dgate Wg + dup Wu, by columns (ffn x tokens) for the weights' gradients. */
+/* What ckpt_gated_backward writes, each or NULL, all with block_rows 1, gradients in either format (one for all), h as CKPT_F8_E4M3: by rows (tokens x ffn) for dx = dgate Wg + dup Wu, by columns (ffn x tokens) for the weights' gradients. */
 typedef struct {
     const ckpt_f8_matrix *dgate, *dup, *dgate_by_col, *dup_by_col, *h_by_col;
 } ckpt_gated_grads;
 
 /* dh = dy Wd, dgate = dh * up * act'(gate), dup = dh * act(gate), h = act(gate) * up, in one pass: dh is never stored. dy is tokens x hidden,
- * w_down by columns ffn x hidden, gate and up tokens x ffn as the forward pass kept them (block_rows 1). */
+ * w_down by columns ffn x hidden (CKPT_F8_E4M3), gate and up tokens x ffn as the forward pass kept them. */
 int ckpt_gated_backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down_by_col, const ckpt_f8_matrix *gate, const ckpt_f8_matrix *up,
                         int32_t activation, const ckpt_gated_grads *grads, void *stream);
 

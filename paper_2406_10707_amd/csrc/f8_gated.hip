@@ -29,6 +29,9 @@ __device__ __forceinline__ float slope_of(float g, float e, float s, float act) 
     else return t == 0 ? s : __builtin_fmaf(t, kGelu * __builtin_fmaf(3 * kCubic * g, g, 1.0f), s);
 }
 
+// Which bytes of a word of four codes stay where `left` columns are left.
+__device__ __forceinline__ uint32_t bytes_kept(int64_t left) { return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1; }
+
 // ------------------------------------------------------------------ forward
 
 struct GatedForward {
@@ -40,7 +43,7 @@ struct GatedForward {
 
 // A tile's columns are 128 of gate and the same 128 of up, in turn groups of 16 TNG, so that a lane has both factors of its elements. The rows' largest values of 128 columns are found among the lanes of a row (q), then
 // through LDS among the WN waves.
-template <class S, int ACT, bool SQUARE, int FA, int FB>
+template <class S, int ACT, bool SQUARE, int FA>
 __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForward p, TileOrder order) {
     static_assert(S::PAIR && S::BN == 256, "a tile has a block of each");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
@@ -49,17 +52,13 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForwa
     const int64_t row = int64_t(t.tm) * S::BM, col = int64_t(t.tn) * 128;
     const F8Loader<S> load(p.x, p.w_gate, p.w_up, p.steps, row, col, lane, wave);
     f32x4 acc[S::TM][S::TN];
-    f8_sums<S, SQUARE, true, FA, FB>(acc, lds, load, 0, p.steps, lane, wm, wn);
+    f8_sums<S, SQUARE, true, FA, 0>(acc, lds, load, 0, p.steps, lane, wm, wn);
     const bool keep = p.gate.codes;
     const int64_t my_col = col + 16 * S::TNG * wn + 4 * S::TNG * q, my_row = row + 16 * S::TM * wm + S::TM * ar;
-    if (col + 128 > p.ffn)      // behind the last column zeros, whatever the last column's values that stand there
+    // columns behind the last are the last again, and change no largest value; their codes are zero (NaN times zero would be none)
+    uint32_t kept[S::TNG];
 #pragma unroll
-        for (int j = 0; j < S::TNG; j++)
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (my_col + 4 * j + e >= p.ffn)
-#pragma unroll
-                    for (int i = 0; i < S::TM; i++) acc[i][j][e] = acc[i][S::TNG + j][e] = 0;
+    for (int j = 0; j < S::TNG; j++) kept[j] = bytes_kept(p.ffn - my_col - 4 * j);
     f32x4 h[S::TM][S::TNG];
     uint32_t *most = reinterpret_cast<uint32_t *>(lds);      // [3][BM][WN]
 #pragma unroll
@@ -102,13 +101,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForwa
             const float inverse = inverses[which * S::BM + 16 * S::TM * wm + S::TM * ar + i];
             uint32_t codes[S::TNG];
 #pragma unroll
-            for (int j = 0; j < S::TNG; j++) codes[j] = f8_codes(value(i, j) * inverse, false);
-            if (col + 128 > p.ffn)      // NaN times zero is no zero
-#pragma unroll
-                for (int j = 0; j < S::TNG; j++) {
-                    const int64_t left = p.ffn - my_col - 4 * j;
-                    codes[j] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-                }
+            for (int j = 0; j < S::TNG; j++) codes[j] = f8_codes(value(i, j) * inverse, false) & kept[j];
             if (my_row + i < p.tokens) {
                 uint8_t *at = to.codes + (my_row + i) * to.code_pitch + my_col;
                 if constexpr (S::TNG == 4) *(u32x4 DSLLM_GLOBAL *)at = u32x4{codes[0], codes[1], codes[2], codes[3]};
@@ -125,13 +118,13 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForwa
 // ------------------------------------------------------------------ up to sixteen tokens
 
 // Rows of `pitch` floats, sixteen a matrix: h, then gate and up
-template <int WAVES, int ACT, int FA, int FB>
+template <int WAVES, int ACT, int FA>
 __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(GatedForward p, float *values, uint64_t pitch) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[F8Few<WAVES, 2>::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = int64_t(blockIdx.x) * 16;
     f32x4 sum[2];
-    F8Few<WAVES, 2>::template sums<FA, FB>(sum, p.x, p.w_gate, p.w_up, p.steps, n0, lds, lane, wave);
+    F8Few<WAVES, 2>::template sums<FA, 0>(sum, p.x, p.w_gate, p.w_up, p.steps, n0, lds, lane, wave);
     if (wave > 0 || (lane & 15) >= p.tokens) return;
     f32x4 h;
 #pragma unroll
@@ -161,149 +154,143 @@ struct GatedBackward {
 // A tile is 128 tokens by 128 columns, a block of each of the forms that are written, and its dh never leaves the registers: dgate, dup and h take their place. A lane has four consecutive rows (TM) of
 // sixteen consecutive columns (TNG): 16 bytes of a row's codes, 4 of a column's. Largest values of rows are found among the lanes of a row (q) and, through LDS, two waves; those of columns among sixteen lanes and two waves.
 // Two blocks share a compute unit, so that the vector work behind a tile's sums runs beside the other's matrix instructions.
-template <int ACT, bool SQUARE, int FA, int FB>
+// One body for whole and ragged tiles (two are 80 KB of code, more than the instruction cache holds): rows and columns past the end are the last ones again. Those columns change no largest value of a row; those rows get factors of zero, and
+// are NaN only where the last row is.
+template <int ACT, bool SQUARE, int FA, bool E5M2>
 __global__ __launch_bounds__(256, 2) void gated_backward_kernel(GatedBackward p, TileOrder order) {
     typedef F8Shape<2, 2, 4, 4, 4, 2, false> S;
+    // largest magnitudes, [640][2]: 128 rows of dgate, of dup, 128 columns of dgate, of dup, of h, each as two waves have seen it; what they are multiplied with, [640]; gate's and up's codes, [32][256]
+    constexpr int DGATE = 0, DUP = 128, DGATE_BY_COL = 256, DUP_BY_COL = 384, H_BY_COL = 512, EVERY = 640;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
+    static_assert(12 * EVERY + 32 * 1024 <= S::BYTES, "");
+    uint32_t *most = reinterpret_cast<uint32_t *>(lds), *parked = most + 3 * EVERY;
+    float *inverses = reinterpret_cast<float *>(lds) + 2 * EVERY;
     const GemmTile t = gemm_tile(order);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, ar = lane & 15;
     const int64_t row = int64_t(t.tm) * 128, col = int64_t(t.tn) * 128;
     const F8Loader<S> load(p.dy, p.w_down, p.w_down, p.steps, row, col, lane, wave);
     f32x4 dgate[4][4], dup[4][4], h[4][4];
-    f8_sums<S, SQUARE, true, FA, FB>(dgate, lds, load, 0, p.steps, lane, wm, wn);
+    f8_sums<S, SQUARE, true, FA, 0>(dgate, lds, load, 0, p.steps, lane, wm, wn);
     const int64_t my_row = row + 64 * wm + 4 * ar, my_col = col + 64 * wn + 16 * q;
-    // largest magnitudes, [640][2]: 128 rows of dgate, of dup, 128 columns of dgate, of dup, of h, each as two waves have seen it; what they are multiplied with, [640]; gate's and up's codes, [32][256]
-    constexpr int DGATE = 0, DUP = 128, DGATE_BY_COL = 256, DUP_BY_COL = 384, H_BY_COL = 512, EVERY = 640;
-    uint32_t *most = reinterpret_cast<uint32_t *>(lds), *parked = most + 4 * EVERY;
-    float *inverses = reinterpret_cast<float *>(lds) + 2 * EVERY;
-    auto finish = [&](auto whole) {
-        float gate_scale[4], up_scale[4];
+    float gate_scale[4], up_scale[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int64_t r = min(my_row + i, p.tokens - 1);
+        const u32x4 gates = *(const u32x4 DSLLM_GLOBAL *)(p.gate.codes + r * p.gate.code_pitch + my_col), ups = *(const u32x4 DSLLM_GLOBAL *)(p.up.codes + r * p.up.code_pitch + my_col);
+        gate_scale[i] = ((const float DSLLM_GLOBAL *)p.gate.scales)[t.tn * p.gate.scale_pitch + r];
+        up_scale[i] = ((const float DSLLM_GLOBAL *)p.up.scales)[t.tn * p.up.scale_pitch + r];
+        if (my_row + i >= p.tokens) gate_scale[i] = up_scale[i] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {      // there are no registers for them
+            parked[(8 * j + i) * 256 + threadIdx.x] = gates[j];
+            parked[(8 * j + 4 + i) * 256 + threadIdx.x] = ups[j];
+        }
+    }
+    float most_dgate[4] = {}, most_dup[4] = {};
+    uint32_t of_column[3] = {};      // of column 16 q + ar of the wave's, of dgate, dup and h
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const int64_t r = whole ? my_row + i : min(my_row + i, p.tokens - 1);      // rows past the end count for nothing below
-            const u32x4 gates = *(const u32x4 DSLLM_GLOBAL *)(p.gate.codes + r * p.gate.code_pitch + my_col), ups = *(const u32x4 DSLLM_GLOBAL *)(p.up.codes + r * p.up.code_pitch + my_col);
-            gate_scale[i] = ((const float DSLLM_GLOBAL *)p.gate.scales)[(col / 128) * p.gate.scale_pitch + r];
-            up_scale[i] = ((const float DSLLM_GLOBAL *)p.up.scales)[(col / 128) * p.up.scale_pitch + r];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {      // there are no registers for them
-                parked[(8 * j + i) * 256 + threadIdx.x] = gates[j];
-                parked[(8 * j + 4 + i) * 256 + threadIdx.x] = ups[j];
-            }
-        }
-        float most_dgate[4] = {}, most_dup[4] = {};
-        uint32_t of_column[3] = {};      // of column 16 q + ar of the wave's, of dgate, dup and h
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const f32x4 g = fp8_values(parked[(8 * j + i) * 256 + threadIdx.x]) * gate_scale[i], u = fp8_values(parked[(8 * j + 4 + i) * 256 + threadIdx.x]) * up_scale[i];
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const float ex = exp_of<ACT>(g[e]), s = sigmoid_of(ex), act = g[e] * s, dh = dgate[i][j][e];
-                    dgate[i][j][e] = dh * u[e] * slope_of<ACT>(g[e], ex, s, act);
-                    dup[i][j][e] = dh * act;
-                    h[i][j][e] = act * u[e];
-                    if (!whole && (my_row + i >= p.tokens || my_col + 4 * j + e >= p.ffn)) dgate[i][j][e] = dup[i][j][e] = h[i][j][e] = 0;
-                }
-                most_dgate[i] = larger(most_dgate[i], dgate[i][j]);
-                most_dup[i] = larger(most_dup[i], dup[i][j]);
-                // these four now: put off, as the compiler would, they need what they are made of as well, and spill
-                asm volatile("" : "+v"(dgate[i][j]), "+v"(dup[i][j]), "+v"(h[i][j]));
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            const f32x4 g = fp8_values(parked[(8 * j + i) * 256 + threadIdx.x]) * gate_scale[i], u = fp8_values(parked[(8 * j + 4 + i) * 256 + threadIdx.x]) * up_scale[i];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                auto column = [&](uint32_t &of, const f32x4 (&v)[4][4]) {
-                    const uint32_t most = most_of_16(bits_of(larger(0, f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]})));
-                    of = ar == 4 * j + e ? most : of;
-                };
-                column(of_column[0], dgate);
-                column(of_column[1], dup);
-                column(of_column[2], h);
-                __builtin_amdgcn_sched_barrier(0);
+                const float ex = exp_of<ACT>(g[e]), s = sigmoid_of(ex), act = g[e] * s, dh = dgate[i][j][e];
+                dgate[i][j][e] = dh * u[e] * slope_of<ACT>(g[e], ex, s, act);
+                dup[i][j][e] = dh * act;
+                h[i][j][e] = act * u[e];
             }
+            // these four now: put off, as the compiler would, they need what they are made of as well, and spill
+            asm volatile("" : "+v"(dgate[i][j]), "+v"(dup[i][j]), "+v"(h[i][j]));
+            most_dgate[i] = larger(most_dgate[i], dgate[i][j]);
+            most_dup[i] = larger(most_dup[i], dup[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int k = 0; k < 3; k++) most[(DGATE_BY_COL + 128 * k + 64 * wn + 16 * q + ar) * 2 + wm] = of_column[k];
+        for (int e = 0; e < 4; e++) {
+            auto column = [&](uint32_t &of, const f32x4 (&v)[4][4]) {
+                const uint32_t found = most_of_16(bits_of(larger(0, f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]})));
+                of = ar == 4 * j + e ? found : of;
+            };
+            column(of_column[0], dgate);
+            column(of_column[1], dup);
+            column(of_column[2], h);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; k++) most[(DGATE_BY_COL + 128 * k + 64 * wn + 16 * q + ar) * 2 + wm] = of_column[k];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t of_dgate = most_of_quarters(bits_of(most_dgate[i])), of_dup = most_of_quarters(bits_of(most_dup[i]));
+        if (q == 0) {
+            most[(DGATE + 64 * wm + 4 * ar + i) * 2 + wn] = of_dgate;
+            most[(DUP + 64 * wm + 4 * ar + i) * 2 + wn] = of_dup;
+        }
+    }
+    __syncthreads();
+    // every scale once: a division is some twenty instructions
+    for (int k = threadIdx.x; k < EVERY; k += 256) {
+        const F8Held &to = k < DUP ? p.dgate : k < DGATE_BY_COL ? p.dup : k < DUP_BY_COL ? p.dgate_by_col : k < H_BY_COL ? p.dup_by_col : p.h_by_col;
+        const float largest = f8_most(E5M2 && k < H_BY_COL);
+        const uint32_t amax = max(most[2 * k], most[2 * k + 1]);
+        inverses[k] = f8_inverse(amax, largest);
+        const int64_t block = k < DGATE_BY_COL ? t.tn : t.tm, of = (k < DGATE_BY_COL ? row : col) + k % 128;
+        if (to.scales && of < to.rows) ((float DSLLM_GLOBAL *)to.scales)[block * to.scale_pitch + of] = f8_scale(amax, largest);
+    }
+    __syncthreads();
+    // codes behind the last element are zero (NaN times zero would be none)
+    uint32_t kept[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) kept[j] = bytes_kept(p.ffn - my_col - 4 * j);
+    auto by_row = [&](const F8Held &to, int first, const f32x4 (&v)[4][4]) {
+        if (!to.codes) return;
+        uint8_t *at = to.codes + my_row * to.code_pitch + my_col;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const uint32_t of_dgate = most_of_quarters(bits_of(most_dgate[i])), of_dup = most_of_quarters(bits_of(most_dup[i]));
-            if (q == 0) {
-                most[(DGATE + 64 * wm + 4 * ar + i) * 2 + wn] = of_dgate;
-                most[(DUP + 64 * wm + 4 * ar + i) * 2 + wn] = of_dup;
-            }
+            const float inverse = inverses[first + 64 * wm + 4 * ar + i];
+            u32x4 codes;
+#pragma unroll
+            for (int j = 0; j < 4; j++) codes[j] = f8_codes(v[i][j] * inverse, E5M2) & kept[j];
+            if (my_row + i < p.tokens) *(u32x4 DSLLM_GLOBAL *)(at + i * to.code_pitch) = codes;
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __syncthreads();
-        // every scale once: a division is some twenty instructions
-        for (int k = threadIdx.x; k < EVERY; k += 256) {
-            const F8Held &to = k < DUP ? p.dgate : k < DGATE_BY_COL ? p.dup : k < DUP_BY_COL ? p.dgate_by_col : k < H_BY_COL ? p.dup_by_col : p.h_by_col;
-            const float largest = f8_most(to.e5m2);
-            const uint32_t amax = max(most[2 * k], most[2 * k + 1]);
-            inverses[k] = f8_inverse(amax, largest);
-            const int64_t block = k < DGATE_BY_COL ? t.tn : t.tm, of = (k < DGATE_BY_COL ? row : col) + k % 128;
-            if (to.scales && of < to.rows) ((float DSLLM_GLOBAL *)to.scales)[block * to.scale_pitch + of] = f8_scale(amax, largest);
-        }
-        __syncthreads();
-        auto by_row = [&](const F8Held &to, int first, const f32x4 (&v)[4][4], auto e5m2) {
-            uint8_t *at = to.codes + my_row * to.code_pitch + my_col;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float inverse = inverses[first + 64 * wm + 4 * ar + i];
-                u32x4 codes;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    codes[j] = f8_codes(v[i][j] * inverse, e5m2);
-                    const int64_t left = p.ffn - my_col - 4 * j;
-                    if (!whole) codes[j] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;      // NaN times zero is no zero
-                }
-                if (whole || my_row + i < p.tokens) *(u32x4 DSLLM_GLOBAL *)(at + i * to.code_pitch) = codes;
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        auto by_col = [&](const F8Held &to, int first, const f32x4 (&v)[4][4], auto e5m2) {
-            const int64_t left = p.tokens - my_row;
-            const uint32_t kept = whole || left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-            uint8_t *at = to.codes + my_col * to.code_pitch + my_row;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const f32x4 inverse = *reinterpret_cast<const f32x4 *>(inverses + first + 64 * wn + 16 * q + 4 * j);
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (whole || my_col + 4 * j + e < p.ffn)
-                        *(uint32_t DSLLM_GLOBAL *)(at + (4 * j + e) * to.code_pitch) = f8_codes(f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]} * inverse[e], e5m2) & kept;
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        // the format is asked once a matrix: branches beside every conversion would spill
-        auto in_format = [&](const F8Held &to, auto write) {
-            if (!to.codes) return;
-            if (to.e5m2) write(std::true_type{});
-            else write(std::false_type{});
-        };
-        in_format(p.dgate, [&](auto e5m2) { by_row(p.dgate, DGATE, dgate, e5m2); });
-        in_format(p.dup, [&](auto e5m2) { by_row(p.dup, DUP, dup, e5m2); });
-        in_format(p.dgate_by_col, [&](auto e5m2) { by_col(p.dgate_by_col, DGATE_BY_COL, dgate, e5m2); });
-        in_format(p.dup_by_col, [&](auto e5m2) { by_col(p.dup_by_col, DUP_BY_COL, dup, e5m2); });
-        if (p.h_by_col.codes) by_col(p.h_by_col, H_BY_COL, h, std::false_type{});
     };
-    if (row + 128 <= p.tokens && col + 128 <= p.ffn) finish(std::true_type{});
-    else finish(std::false_type{});
+    const uint32_t rows_kept = bytes_kept(p.tokens - my_row);
+    auto by_col = [&](const F8Held &to, int first, const f32x4 (&v)[4][4], bool e5m2) {
+        if (!to.codes) return;
+        uint8_t *at = to.codes + my_col * to.code_pitch + my_row;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const f32x4 inverse = *reinterpret_cast<const f32x4 *>(inverses + first + 64 * wn + 16 * q + 4 * j);
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (my_col + 4 * j + e < p.ffn)
+                    *(uint32_t DSLLM_GLOBAL *)(at + (4 * j + e) * to.code_pitch) = f8_codes(f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]} * inverse[e], e5m2) & rows_kept;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    by_row(p.dgate, DGATE, dgate);
+    by_row(p.dup, DUP, dup);
+    by_col(p.dgate_by_col, DGATE_BY_COL, dgate, E5M2);
+    by_col(p.dup_by_col, DUP_BY_COL, dup, E5M2);
+    by_col(p.h_by_col, H_BY_COL, h, false);
 }
 
 // ------------------------------------------------------------------ host
 
 template <class F>
-void with_kinds(int32_t activation, bool a_e5m2, bool b_e5m2, F f) {
-    auto with_b = [&](auto act, auto fa) {
-        if (b_e5m2) f(act, fa, std::integral_constant<int, 1>());
-        else f(act, fa, std::integral_constant<int, 0>());
+void with_kinds(int32_t activation, bool e5m2, bool square, F f) {
+    auto with_square = [&](auto act, auto fa) {
+        if (square) f(act, fa, std::true_type());
+        else f(act, fa, std::false_type());
     };
-    auto with_a = [&](auto act) {
-        if (a_e5m2) with_b(act, std::integral_constant<int, 1>());
-        else with_b(act, std::integral_constant<int, 0>());
+    auto with_format = [&](auto act) {
+        if (e5m2) with_square(act, std::integral_constant<int, 1>());
+        else with_square(act, std::integral_constant<int, 0>());
     };
-    if (activation == CKPT_GATE_SILU) with_a(std::integral_constant<int, CKPT_GATE_SILU>());
-    else with_a(std::integral_constant<int, CKPT_GATE_GELU>());
+    if (activation == CKPT_GATE_SILU) with_format(std::integral_constant<int, CKPT_GATE_SILU>());
+    else with_format(std::integral_constant<int, CKPT_GATE_GELU>());
 }
 
 // Sides are at most 2^31 - 1; the product of tiles is at most 2^24 - 1, so that a grid has fewer than 2^32 work-items.
@@ -335,7 +322,8 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
             if (const char *why = wrong_f8_matrix(e.m, ranges)) return refuse(CKPT_EINVAL, std::string(e.name) + why);
     for (int i = 0; i < 3; i++)
         if (const char *why = wrong_f8_contraction(every[i].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + why);
-    if (w_gate->format != w_up->format || w_gate->block_rows != w_up->block_rows || w_gate->rows != w_up->rows) return refuse(CKPT_EINVAL, "w_gate and w_up differ in format, block_rows or rows");
+    if (w_gate->format != CKPT_F8_E4M3 || w_up->format != CKPT_F8_E4M3) return refuse(CKPT_EINVAL, "w_gate and w_up must be CKPT_F8_E4M3");
+    if (w_gate->block_rows != w_up->block_rows || w_gate->rows != w_up->rows) return refuse(CKPT_EINVAL, "w_gate and w_up differ in block_rows or rows");
     if (w_gate->cols != x->cols || w_up->cols != x->cols) return refuse(CKPT_EINVAL, "x and the weights differ in their columns");
     const int64_t tokens = x->rows, ffn = w_gate->rows;
     if (tokens > 0x7FFFFFFF || ffn > 0x7FFFFFFF) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1");
@@ -349,15 +337,15 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
     if (tokens == 0 || ffn == 0) return CKPT_OK;
     const uint32_t steps = f8_steps(uint64_t(x->cols));
     const GatedForward p{f8_side(x), f8_side(w_gate), f8_side(w_up), F8Held(gate), F8Held(up), F8Held(h), tokens, ffn, steps};
-    const bool a_e5m2 = x->format == CKPT_F8_E5M2, b_e5m2 = w_gate->format == CKPT_F8_E5M2;
+    const bool x_e5m2 = x->format == CKPT_F8_E5M2;
     const int64_t across = (ffn + 127) / 128;
     if (tokens <= 16 && steps && workspace && workspace_bytes >= few_bytes(ffn) && across < 1 << 20) {
         if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
         if (const char *why = ranges.wrong(workspace, few_bytes(ffn))) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
         float *values = static_cast<float *>(workspace);
         const uint64_t pitch = few_pitch(ffn);
-        with_kinds(activation, a_e5m2, b_e5m2, [&](auto act, auto fa, auto fb) {
-            hipLaunchKernelGGL((gated_few_kernel<4, act, fa, fb>), dim3(unsigned((ffn + 15) / 16)), dim3(256), 0, stream, p, values, pitch);
+        with_kinds(activation, x_e5m2, true, [&](auto act, auto fa, auto) {
+            hipLaunchKernelGGL((gated_few_kernel<4, act, fa>), dim3(unsigned((ffn + 15) / 16)), dim3(256), 0, stream, p, values, pitch);
         });
         hipLaunchKernelGGL(gated_round_kernel, dim3(unsigned((ffn + 511) / 512), gate ? 3 : 1), dim3(256), 0, stream, p, values, pitch);
         return launched();
@@ -368,10 +356,7 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
         if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, "more than 2^22 tiles of tokens and columns");
         const dim3 grid(unsigned(down * across)), block(S::THREADS);
         const TileOrder order(uint32_t(down), uint32_t(across), true);
-        with_kinds(activation, a_e5m2, b_e5m2, [&](auto act, auto fa, auto fb) {
-            if (p.w_gate.shift) hipLaunchKernelGGL((gated_forward_kernel<S, act, true, fa, fb>), grid, block, 0, stream, p, order);
-            else hipLaunchKernelGGL((gated_forward_kernel<S, act, false, fa, fb>), grid, block, 0, stream, p, order);
-        });
+        with_kinds(activation, x_e5m2, p.w_gate.shift, [&](auto act, auto fa, auto square) { hipLaunchKernelGGL((gated_forward_kernel<S, act, square, fa>), grid, block, 0, stream, p, order); });
         return launched();
     };
     switch (gated_form(uint64_t(tokens), uint64_t(across))) {
@@ -396,6 +381,14 @@ int backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down, const ckpt_
     if (!any) return refuse(CKPT_EINVAL, "nothing is asked for");
     for (int i = 0; i < 2; i++)
         if (const char *why = wrong_f8_contraction(every[i].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + why);
+    if (w_down->format != CKPT_F8_E4M3) return refuse(CKPT_EINVAL, "w_down_by_col must be CKPT_F8_E4M3");
+    int32_t format = 0;
+    for (int i = 4; i < 8; i++)
+        if (every[i].m) {
+            if (format && every[i].m->format != format) return refuse(CKPT_EINVAL, "the gradients differ in their format");
+            format = every[i].m->format;
+        }
+    const bool e5m2 = format == CKPT_F8_E5M2;
     if (dy->cols != w_down->cols) return refuse(CKPT_EINVAL, "dy and w_down_by_col differ in their columns");
     const int64_t tokens = dy->rows, ffn = w_down->rows;
     if (tokens > 0x7FFFFFFF || ffn > 0x7FFFFFFF) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1");
@@ -414,9 +407,9 @@ int backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down, const ckpt_
     if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, "more than 2^22 tiles of tokens and columns");
     const dim3 grid(unsigned(down * across));
     const TileOrder order(uint32_t(down), uint32_t(across), true);
-    with_kinds(activation, dy->format == CKPT_F8_E5M2, w_down->format == CKPT_F8_E5M2, [&](auto act, auto fa, auto fb) {
-        if (p.w_down.shift) hipLaunchKernelGGL((gated_backward_kernel<act, true, fa, fb>), grid, dim3(256), 0, stream, p, order);
-        else hipLaunchKernelGGL((gated_backward_kernel<act, false, fa, fb>), grid, dim3(256), 0, stream, p, order);
+    with_kinds(activation, dy->format == CKPT_F8_E5M2, p.w_down.shift, [&](auto act, auto fa, auto square) {
+        if (e5m2) hipLaunchKernelGGL((gated_backward_kernel<act, square, fa, true>), grid, dim3(256), 0, stream, p, order);
+        else hipLaunchKernelGGL((gated_backward_kernel<act, square, fa, false>), grid, dim3(256), 0, stream, p, order);
     });
     return launched();
 }

@@ -31,12 +31,11 @@ struct F8Shape {
 
 __device__ __forceinline__ uint32_t f8_rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
 
-// Rows past the end of a matrix lie past the descriptor's end, so that they are not read; what LDS has in their places counts for nothing that is stored. (The scalar offset, the step's, counts or does not count in that check: a row inside is inside
-// either way, the next row's first byte is outside.) Their scales are the last row's.
+// Rows past the end of a matrix are its last row again.
 template <class S>
 struct F8Loader {
     __amdgpu_buffer_rsrc_t ra, rb[2];
-    uint32_t pitch_a, pitch_b[2], row_a, row_b, piece, wave;      // this lane's rows with the wave's first load, and what part of a row
+    uint32_t pitch_a, pitch_b[2], row_a, row_b, last_a, last_b, piece, wave;      // this lane's rows with the wave's first load, and what part of a row
     const float *scale;
     uint64_t scale_pitch;
 
@@ -48,7 +47,8 @@ struct F8Loader {
 
     __device__ __forceinline__ F8Loader(const F8Side a, const F8Side b, const F8Side b2, uint32_t steps, int64_t row, int64_t col, int lane, uint32_t wave_) : wave(wave_) {
         constexpr int ROWS_B = S::PAIR ? S::BN / 2 : S::BN;
-        const uint32_t last_a = uint32_t(min(a.rows - row, int64_t(S::BM)) - 1), last_b = uint32_t(min(b.rows - col, int64_t(ROWS_B)) - 1);
+        last_a = uint32_t(min(a.rows - row, int64_t(S::BM)) - 1);
+        last_b = uint32_t(min(b.rows - col, int64_t(ROWS_B)) - 1);
         // a load's places are those of the first load and a multiple of 8 NW: sizes are powers of two, so that its rows are the sum of both places' rows
         const uint32_t place = 8 * wave + (lane >> 3);
         row_a = row_of_place_a(place);
@@ -90,10 +90,10 @@ struct F8Loader {
     }
     __device__ __forceinline__ void issue(uint8_t *stage, uint32_t step, int c) const {
         if (c < S::LA) {
-            const uint32_t at = (row_a + row_of_place_a(8 * S::NW * c)) * pitch_a + piece;
+            const uint32_t at = min(row_a + row_of_place_a(8 * S::NW * c), last_a) * pitch_a + piece;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (DSLLM_LDS void *)(stage + 1024 * (S::NW * c + wave)), 16, at, 128 * step, 0, 0);
         } else if (c < S::LA + S::LB) {
-            const uint32_t first = 8 * S::NW * (c - S::LA), which = matrix_of(first), at = (row_b + row_of(row_of_place_b(first))) * pitch_b[which] + piece;
+            const uint32_t first = 8 * S::NW * (c - S::LA), which = matrix_of(first), at = min(row_b + row_of(row_of_place_b(first)), last_b) * pitch_b[which] + piece;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[which], (DSLLM_LDS void *)(stage + S::BM * 128 + 1024 * (S::NW * (c - S::LA) + wave)), 16, at, 128 * step, 0, 0);
         } else __builtin_amdgcn_global_load_lds((const DSLLM_GLB void *)(scale + step * scale_pitch), (DSLLM_LDS void *)(stage + S::CODES + 256 * wave), 4, 0, 0);
     }

@@ -64,7 +64,7 @@ FORWARD = [(1, 64, 128), (1, 100, 37), (2, 4096, 256), (7, 513, 300), (16, 640, 
 @pytest.mark.parametrize("keep", [False, True])
 def test_forward(keep, name):
     for case, (t, d, f) in enumerate(FORWARD):
-        fx, fw = [(fo.E4M3, fo.E4M3), (fo.E5M2, fo.E4M3), (fo.E4M3, fo.E5M2)][case % 3]
+        fx, fw = [(fo.E4M3, fo.E4M3), (fo.E5M2, fo.E4M3)][case % 2]
         check_forward(t, d, f, name, keep, fx, fw, (128, 1)[case // 2 % 2], case)
 
 
@@ -100,7 +100,7 @@ def test_backward(fdy, name):
         rng = np.random.default_rng(case)
         dy, wd = Given(rows_of(rng, (t, d), 2.0), fdy, wider=case % 2), Given((rng.standard_normal((f, d)) / d ** 0.5).astype(np.float32), fo.E4M3, (128, 1)[case % 2])
         gate, up = Given(rows_of(rng, (t, f)), wider=case % 3), Given(rows_of(rng, (t, f)), wider=(case + 1) % 3)
-        formats = [(fdy, fdy), (fo.E5M2, fo.E4M3)][case % 2]
+        formats = [(fdy, fdy), (fo.E5M2, fo.E5M2), (fo.E4M3, fo.E4M3)][case % 3]
         out = run_backward(dy, wd, gate.on, up.on, name, formats, wider=case % 2)
         want = fo.backward(dy.v, wd.v, gate.v, up.v, name)
         for k, m in out.items():
