@@ -44,12 +44,9 @@ struct GatedForward {
 // A tile's columns are 128 of gate and the same 128 of up, in turn groups of 16 TNG, so that a lane has both factors of its elements. The rows' largest values of 128 columns are found among the lanes of a row (q), then
 // through LDS among the WN waves.
 template <class S, int ACT, bool SQUARE, int FA>
-__global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForward p, TileOrder order) {
+__device__ __forceinline__ void gated_forward_tile(const GatedForward &p, uint8_t *lds, int64_t row, int64_t col) {
     static_assert(S::PAIR && S::BN == 256, "a tile has a block of each");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
-    const GemmTile t = gemm_tile(order);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, ar = lane & 15;
-    const int64_t row = int64_t(t.tm) * S::BM, col = int64_t(t.tn) * 128;
     const F8Loader<S> load(p.x, p.w_gate, p.w_up, p.steps, row, col, lane, wave);
     f32x4 acc[S::TM][S::TN];
     f8_sums<S, SQUARE, true, FA, 0>(acc, lds, load, 0, p.steps, lane, wm, wn);
@@ -115,6 +112,25 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForwa
     out(p.up, 2, [&](int i, int j) { return acc[i][S::TNG + j]; });
 }
 
+template <class S, int ACT, bool SQUARE, int FA>
+__global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForward p, TileOrder order) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
+    const GemmTile t = gemm_tile(order);
+    gated_forward_tile<S, ACT, SQUARE, FA>(p, lds, int64_t(t.tm) * S::BM, int64_t(t.tn) * 128);
+}
+
+// Tiles of 256 tokens up to the `whole`th block; behind them each two blocks take the halves of one, where the last round of blocks would leave half of the chip idle: 4096 tokens, 4096 to 11008, 5.4 rounds, 629 -> 603 us.
+template <int ACT, bool SQUARE, int FA>
+__global__ __launch_bounds__(512, 2) void gated_forward_halves_kernel(GatedForward p, TileOrder order, uint32_t whole) {
+    typedef F8Shape<4, 2, 4, 8, 4, 2, true> S;
+    typedef F8Shape<4, 2, 2, 8, 4, 2, true> Half;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
+    const uint32_t rest = (gridDim.x - whole) / 2, second = blockIdx.x >= whole + rest;
+    const GemmTile t = gemm_tile(order, second ? blockIdx.x - rest : blockIdx.x);
+    if (blockIdx.x < whole) gated_forward_tile<S, ACT, SQUARE, FA>(p, lds, int64_t(t.tm) * 256, int64_t(t.tn) * 128);
+    else if (int64_t(t.tm) * 256 + 128 * second < p.tokens) gated_forward_tile<Half, ACT, SQUARE, FA>(p, lds, int64_t(t.tm) * 256 + 128 * second, int64_t(t.tn) * 128);
+}
+
 // ------------------------------------------------------------------ up to sixteen tokens
 
 // Rows of `pitch` floats, sixteen a matrix: h, then gate and up
@@ -170,20 +186,25 @@ __global__ __launch_bounds__(256, 2) void gated_backward_kernel(GatedBackward p,
     const int64_t row = int64_t(t.tm) * 128, col = int64_t(t.tn) * 128;
     const F8Loader<S> load(p.dy, p.w_down, p.w_down, p.steps, row, col, lane, wave);
     f32x4 dgate[4][4], dup[4][4], h[4][4];
-    f8_sums<S, SQUARE, true, FA, 0>(dgate, lds, load, 0, p.steps, lane, wm, wn);
     const int64_t my_row = row + 64 * wm + 4 * ar, my_col = col + 64 * wn + 16 * q;
+    u32x4 gates[4], ups[4];
     float gate_scale[4], up_scale[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const int64_t r = min(my_row + i, p.tokens - 1);
-        const u32x4 gates = *(const u32x4 DSLLM_GLOBAL *)(p.gate.codes + r * p.gate.code_pitch + my_col), ups = *(const u32x4 DSLLM_GLOBAL *)(p.up.codes + r * p.up.code_pitch + my_col);
+        gates[i] = *(const u32x4 DSLLM_GLOBAL *)(p.gate.codes + r * p.gate.code_pitch + my_col);
+        ups[i] = *(const u32x4 DSLLM_GLOBAL *)(p.up.codes + r * p.up.code_pitch + my_col);
         gate_scale[i] = ((const float DSLLM_GLOBAL *)p.gate.scales)[t.tn * p.gate.scale_pitch + r];
         up_scale[i] = ((const float DSLLM_GLOBAL *)p.up.scales)[t.tn * p.up.scale_pitch + r];
+    }
+    f8_sums<S, SQUARE, true, FA, 0>(dgate, lds, load, 0, p.steps, lane, wm, wn);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
         if (my_row + i >= p.tokens) gate_scale[i] = up_scale[i] = 0;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {      // there are no registers for them
-            parked[(8 * j + i) * 256 + threadIdx.x] = gates[j];
-            parked[(8 * j + 4 + i) * 256 + threadIdx.x] = ups[j];
+        for (int j = 0; j < 4; j++) {      // there are no registers for them any more
+            parked[(8 * j + i) * 256 + threadIdx.x] = gates[i][j];
+            parked[(8 * j + 4 + i) * 256 + threadIdx.x] = ups[i][j];
         }
     }
     float most_dgate[4] = {}, most_dup[4] = {};
@@ -360,7 +381,14 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
         return launched();
     };
     switch (gated_form(uint64_t(tokens), uint64_t(across))) {
-        case 0: return tiles(F8Shape<4, 2, 4, 8, 4, 2, true>());
+        case 0: {
+            const int64_t down = (tokens + 255) / 256, count = down * across, rest = count % kF8Units;
+            if (!fits_grid(down, across) || rest == 0 || 2 * rest > kF8Units) return tiles(F8Shape<4, 2, 4, 8, 4, 2, true>());
+            with_kinds(activation, x_e5m2, p.w_gate.shift, [&](auto act, auto fa, auto square) {
+                hipLaunchKernelGGL((gated_forward_halves_kernel<act, square, fa>), dim3(unsigned(count + rest)), dim3(512), 0, stream, p, TileOrder(uint32_t(down), uint32_t(across), true), uint32_t(count - rest));
+            });
+            return launched();
+        }
         case 1: return tiles(F8Shape<4, 2, 2, 8, 4, 2, true>());
         default: return tiles(F8Shape<2, 4, 2, 4, 2, 2, true>());
     }

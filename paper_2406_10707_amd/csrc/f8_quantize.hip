@@ -20,6 +20,12 @@ __global__ __launch_bounds__(256) void f8_rows_kernel(F8Source src, F8Held to, u
 
 // ------------------------------------------------------------------ tiles: columns, both forms, blocks of 128 x 128
 
+template <class F>
+__device__ __forceinline__ void for_each_of_eight(F f) {
+    f(std::integral_constant<int, 0>()); f(std::integral_constant<int, 1>()); f(std::integral_constant<int, 2>()); f(std::integral_constant<int, 3>());
+    f(std::integral_constant<int, 4>()); f(std::integral_constant<int, 5>()); f(std::integral_constant<int, 6>()); f(std::integral_constant<int, 7>());
+}
+
 // Word i of four, each with four bytes, becomes the four words' bytes i.
 __device__ __forceinline__ u32x4 transposed(u32x4 v) {
     const uint32_t ab_lo = __builtin_amdgcn_perm(v.y, v.x, 0x05010400), ab_hi = __builtin_amdgcn_perm(v.y, v.x, 0x07030602);      // x0 y0 x1 y1, x2 y2 x3 y3
@@ -28,36 +34,44 @@ __device__ __forceinline__ u32x4 transposed(u32x4 v) {
                  __builtin_amdgcn_perm(cd_hi, ab_hi, 0x07060302)};
 }
 
-// A tile of 128 x 128 elements, which stays in registers: a thread has eight by eight of them, sixteen lanes across, four groups of eight rows a wave. The rows' largest values are found among sixteen lanes, the columns' among
-// a wave's four groups and, through LDS, the four waves. The columns' codes go through LDS as bytes (128 columns of 128, and 16 more so that neighbouring columns begin in different banks), so that a
-// store is whole lines. SQUARE: one scale for the tile, so that both forms have the same codes. Bound by memory.
+// A tile of 128 x 128 elements, which stays in registers: a thread has eight rows of eight columns (of an f32 source twice four, half a tile apart: its loads are sixteen bytes of neighbouring lanes), sixteen lanes across, four groups of
+// eight rows a wave. The rows' largest values are found among sixteen lanes, the columns' among a wave's four groups and, through LDS, the four waves; a scale is found by one lane (its two divisions are some 25 instructions) and
+// handed to the others. The columns' codes go through LDS as bytes (128 columns of 128, and 16 more so that neighbouring columns begin in different banks), so that a store is whole lines. SQUARE: one scale for the tile, so that both forms
+// have the same codes. Bound by memory.
 template <int SRC, bool BY_ROW, bool BY_COL, bool SQUARE>
 __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_row, F8Held by_col, uint32_t across_tiles) {
-    constexpr bool HELD = SRC == kHeld, KEPT = HELD && SQUARE;      // KEPT: codes and scales move as they are
+    constexpr bool HELD = SRC == kHeld, KEPT = HELD && SQUARE, APART = SRC == CKPT_F32;      // KEPT: codes and scales move as they are
     constexpr int PITCH = 128 + 16;
     __shared__ __attribute__((aligned(16))) uint8_t turned[BY_COL ? 128 * PITCH : 16];
-    __shared__ uint32_t most_of_wave[4][128];
+    __shared__ __attribute__((aligned(16))) uint32_t most_of_wave[4][128];      // then what columns are multiplied with
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, across = threadIdx.x & 15, down = threadIdx.x >> 4;
     const uint32_t tile_down = blockIdx.x / across_tiles, tile_across = blockIdx.x - tile_down * across_tiles;
-    const int64_t row0 = 128 * int64_t(tile_down) + 8 * down, col0 = 128 * int64_t(tile_across), col = col0 + 8 * across;
+    const int64_t row0 = 128 * int64_t(tile_down) + 8 * down, col0 = 128 * int64_t(tile_across);
+    const uint32_t in_lo = APART ? 4 * across : 8 * across, in_hi = APART ? 64 + 4 * across : 8 * across + 4;      // the thread's columns: four and four
+    const int64_t col_lo = col0 + in_lo, col_hi = col0 + in_hi;
     const bool whole = 128 * int64_t(tile_down) + 128 <= src.rows && col0 + 128 <= src.cols;      // loads without conditions: all are under way before the first is waited for
-    const uint32_t count = col < src.cols ? uint32_t(min(src.cols - col, int64_t(8))) : 0;
+    auto left_of = [&](int64_t col) { return col < src.cols ? uint32_t(min(src.cols - col, int64_t(4))) : 0; };
+    const uint32_t count_lo = left_of(col_lo), count_hi = left_of(col_hi), rows_left = uint32_t(max(int64_t(0), min(src.rows - row0, int64_t(8))));
     f32x4 lo[8], hi[8];
     u32x2 codes[8];
     if constexpr (HELD) {
-        const uint8_t *at = src.at + row0 * src.ld + col;      // a row's codes reach to a multiple of 128
+        const uint8_t *at = src.at + row0 * src.ld + col_lo;      // a row's codes reach to a multiple of 128
+        const float DSLLM_GLOBAL *scales = (const float DSLLM_GLOBAL *)src.scales + tile_across * src.scale_pitch + row0;
         float scale[8];
         if (whole) {
 #pragma unroll
             for (int i = 0; i < 8; i++) codes[i] = *(const u32x2 DSLLM_GLOBAL *)(at + i * src.ld);
-            if constexpr (!KEPT)
+            if constexpr (!KEPT) {
+                typedef f32x4 four_aligned4 __attribute__((aligned(4)));
+                const f32x4 upper = *(const four_aligned4 DSLLM_GLOBAL *)scales, lower = *(const four_aligned4 DSLLM_GLOBAL *)(scales + 4);
 #pragma unroll
-                for (int i = 0; i < 8; i++) scale[i] = ((const float DSLLM_GLOBAL *)src.scales)[tile_across * src.scale_pitch + row0 + i];
+                for (int i = 0; i < 4; i++) { scale[i] = upper[i]; scale[4 + i] = lower[i]; }
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 codes[i] = row0 + i < src.rows ? *(const u32x2 DSLLM_GLOBAL *)(at + i * src.ld) : u32x2{0, 0};
-                if constexpr (!KEPT) scale[i] = row0 + i < src.rows ? ((const float DSLLM_GLOBAL *)src.scales)[tile_across * src.scale_pitch + row0 + i] : 0;
+                if constexpr (!KEPT) scale[i] = row0 + i < src.rows ? scales[i] : 0;
             }
         }
         if constexpr (!KEPT)
@@ -66,16 +80,31 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
                 lo[i] = f8_values(codes[i].x, src.e5m2) * scale[i];
                 hi[i] = f8_values(codes[i].y, src.e5m2) * scale[i];
             }
+    } else if constexpr (APART) {
+        const float *at = reinterpret_cast<const float *>(src.at) + row0 * src.ld + col_lo;
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                lo[i] = load4<SRC>(at + i * src.ld);
+                hi[i] = load4<SRC>(at + i * src.ld + 64);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                lo[i] = load_upto4<SRC>(at + i * src.ld, row0 + i < src.rows ? count_lo : 0);
+                hi[i] = load_upto4<SRC>(at + i * src.ld + 64, row0 + i < src.rows ? count_hi : 0);
+            }
+        }
     } else {
         constexpr uint32_t kBytes = sizeof(typename Element<SRC>::one);
-        const uint8_t *at = src.at + (row0 * src.ld + col) * kBytes;
+        const uint8_t *at = src.at + (row0 * src.ld + col_lo) * kBytes;
         Eight<SRC> x[8];
         if (whole) {
 #pragma unroll
             for (int i = 0; i < 8; i++) x[i].load(at + i * src.ld * kBytes);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i].load_upto(at + i * src.ld * kBytes, row0 + i < src.rows ? count : 0);
+            for (int i = 0; i < 8; i++) x[i].load_upto(at + i * src.ld * kBytes, row0 + i < src.rows ? count_lo + count_hi : 0);
         }
 #pragma unroll
         for (int i = 0; i < 8; i++) {
@@ -83,46 +112,55 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
             hi[i] = __builtin_convertvector(x[i].hi, f32x4);
         }
     }
-    // behind the last row and column zeros, whatever the block's scale
-    auto inside = [&](u32x2 c, int64_t left, uint32_t n) {
-        if (whole) return c;
-        const uint64_t kept = left <= 0 ? 0 : n >= 8 ? ~0ull : (1ull << (8 * n)) - 1;
-        return u32x2{c.x & uint32_t(kept), c.y & uint32_t(kept >> 32)};
+    auto bytes_kept = [](uint32_t n) { return n >= 4 ? ~0u : (1u << (8 * n)) - 1; };
+    const uint32_t kept_lo = bytes_kept(count_lo), kept_hi = bytes_kept(count_hi);      // codes behind the last element are zero, whatever the block's scale
+    auto put_row = [&](int i, u32x2 c) {
+        if (!whole && row0 + i >= src.rows) return;
+        uint8_t *at = by_row.codes + (row0 + i) * by_row.code_pitch + col_lo;
+        if constexpr (APART) {
+            __builtin_nontemporal_store(c.x, (uint32_t DSLLM_GLOBAL *)at);
+            __builtin_nontemporal_store(c.y, (uint32_t DSLLM_GLOBAL *)(at + 64));
+        } else __builtin_nontemporal_store(c, (u32x2 DSLLM_GLOBAL *)at);
     };
-    uint32_t amax = 0;
-    float inverse = 0;
     if constexpr (SQUARE && !KEPT) {
         float largest = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) largest = larger(larger(largest, lo[i]), hi[i]);
-        amax = most_of_quarters(most_of_16(bits_of(largest)));
+        uint32_t amax = most_of_quarters(most_of_16(bits_of(largest)));
         if (lane == 0) most_of_wave[wave][0] = amax;
         __syncthreads();
         amax = max(max(most_of_wave[0][0], most_of_wave[1][0]), max(most_of_wave[2][0], most_of_wave[3][0]));
         const bool e5m2 = BY_ROW ? by_row.e5m2 : by_col.e5m2;
-        inverse = f8_inverse(amax, f8_most(e5m2));
+        const float inverse = f8_inverse(amax, f8_most(e5m2));
 #pragma unroll
-        for (int i = 0; i < 8; i++) codes[i] = inside(u32x2{f8_codes(lo[i] * inverse, e5m2), f8_codes(hi[i] * inverse, e5m2)}, src.rows - row0 - i, count);
+        for (int i = 0; i < 8; i++) {
+            codes[i] = u32x2{f8_codes(lo[i] * inverse, e5m2) & kept_lo, f8_codes(hi[i] * inverse, e5m2) & kept_hi};
+            if (!whole && row0 + i >= src.rows) codes[i] = u32x2{0, 0};
+        }
         if (threadIdx.x == 0) {
             const float scale = f8_scale(amax, f8_most(e5m2));
             if constexpr (BY_ROW) ((float DSLLM_GLOBAL *)by_row.scales)[tile_across * by_row.scale_pitch + tile_down] = scale;
             if constexpr (BY_COL) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + tile_across] = scale;
         }
+        if constexpr (BY_ROW)
+#pragma unroll
+            for (int i = 0; i < 8; i++) put_row(i, codes[i]);
     }
     if constexpr (KEPT)
         if (threadIdx.x == 0) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + tile_across] = ((const float DSLLM_GLOBAL *)src.scales)[tile_across * src.scale_pitch + tile_down];
-    if constexpr (BY_ROW) {
+    if constexpr (BY_ROW && !SQUARE) {
+        uint32_t amax = 0;      // of row `across` of the eight
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            u32x2 c = codes[i];
-            if constexpr (!SQUARE) {
-                amax = most_of_16(bits_of(larger(larger(0, lo[i]), hi[i])));
-                inverse = f8_inverse(amax, f8_most(by_row.e5m2));
-                c = inside(u32x2{f8_codes(lo[i] * inverse, by_row.e5m2), f8_codes(hi[i] * inverse, by_row.e5m2)}, src.rows - row0 - i, count);
-                if (across == i && (whole || row0 + i < src.rows)) ((float DSLLM_GLOBAL *)by_row.scales)[tile_across * by_row.scale_pitch + row0 + i] = f8_scale(amax, f8_most(by_row.e5m2));
-            }
-            if (whole || row0 + i < src.rows) __builtin_nontemporal_store(c, (u32x2 DSLLM_GLOBAL *)(by_row.codes + (row0 + i) * by_row.code_pitch + col));
+            const uint32_t found = most_of_16(bits_of(larger(larger(0, lo[i]), hi[i])));
+            amax = across == uint32_t(i) ? found : amax;
         }
+        const float mine = f8_inverse(amax, f8_most(by_row.e5m2));
+        if (across < 8 && row0 + across < src.rows) ((float DSLLM_GLOBAL *)by_row.scales)[tile_across * by_row.scale_pitch + row0 + across] = f8_scale(amax, f8_most(by_row.e5m2));
+        for_each_of_eight([&](auto i) {
+            const float inverse = of_lane_of_16<i>(mine);
+            put_row(i, u32x2{f8_codes(lo[i] * inverse, by_row.e5m2) & kept_lo, f8_codes(hi[i] * inverse, by_row.e5m2) & kept_hi});
+        });
     }
     if constexpr (BY_COL) {
         if constexpr (!SQUARE) {
@@ -130,38 +168,34 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
 #pragma unroll
             for (int j = 0; j < 8; j++) {
                 auto at = [&](int i) { return j < 4 ? lo[i][j & 3] : hi[i][j & 3]; };
-                most[j] = bits_of(larger(larger(0, f32x4{at(0), at(1), at(2), at(3)}), f32x4{at(4), at(5), at(6), at(7)}));
+                most[j] = most_of_quarters(bits_of(larger(larger(0, f32x4{at(0), at(1), at(2), at(3)}), f32x4{at(4), at(5), at(6), at(7)})));
             }
-#pragma unroll
-            for (int j = 0; j < 8; j++) {
-                most[j] = most_of_quarters(most[j]);
-                if (lane < 16) most_of_wave[wave][8 * across + j] = most[j];
+            if (lane < 16) {
+                *reinterpret_cast<u32x4 *>(&most_of_wave[wave][in_lo]) = u32x4{most[0], most[1], most[2], most[3]};
+                *reinterpret_cast<u32x4 *>(&most_of_wave[wave][in_hi]) = u32x4{most[4], most[5], most[6], most[7]};
             }
             __syncthreads();
-#pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const uint32_t c = 8 * across + j;
-                most[j] = max(max(most_of_wave[0][c], most_of_wave[1][c]), max(most_of_wave[2][c], most_of_wave[3][c]));
+            if (threadIdx.x < 128) {
+                const uint32_t c = threadIdx.x, amax = max(max(most_of_wave[0][c], most_of_wave[1][c]), max(most_of_wave[2][c], most_of_wave[3][c]));
+                most_of_wave[0][c] = __float_as_uint(f8_inverse(amax, f8_most(by_col.e5m2)));
+                if (col0 + c < src.cols) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + col0 + c] = f8_scale(amax, f8_most(by_col.e5m2));
             }
+            __syncthreads();
+            const f32x4 by_lo = *reinterpret_cast<const f32x4 *>(&most_of_wave[0][in_lo]), by_hi = *reinterpret_cast<const f32x4 *>(&most_of_wave[0][in_hi]);
+            const uint32_t upper = bytes_kept(rows_left), lower = bytes_kept(rows_left > 4 ? rows_left - 4 : 0);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                const float by = f8_inverse(most[j], f8_most(by_col.e5m2));
-                f32x4 a, b;
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    a[i] = (j < 4 ? lo[i][j & 3] : hi[i][j & 3]) * by;
-                    b[i] = (j < 4 ? lo[i + 4][j & 3] : hi[i + 4][j & 3]) * by;
-                }
-                const u32x2 c = inside(u32x2{f8_codes(a, by_col.e5m2), f8_codes(b, by_col.e5m2)}, int64_t(count) - j, uint32_t(max(int64_t(0), min(src.rows - row0, int64_t(8)))));
-                *reinterpret_cast<u32x2 *>(turned + (8 * across + j) * PITCH + 8 * down) = c;
-                if (down == j && (whole || j < int(count))) ((float DSLLM_GLOBAL *)by_col.scales)[tile_down * by_col.scale_pitch + col + j] = f8_scale(most[j], f8_most(by_col.e5m2));
+                auto at = [&](int i) { return j < 4 ? lo[i][j & 3] : hi[i][j & 3]; };
+                const float by = j < 4 ? by_lo[j & 3] : by_hi[j & 3];
+                *reinterpret_cast<u32x2 *>(turned + ((j < 4 ? in_lo : in_hi) + (j & 3)) * PITCH + 8 * down) =
+                    u32x2{f8_codes(f32x4{at(0), at(1), at(2), at(3)} * by, by_col.e5m2) & upper, f8_codes(f32x4{at(4), at(5), at(6), at(7)} * by, by_col.e5m2) & lower};
             }
         } else {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {      // columns 4 h to 4 h + 3
+            for (int h = 0; h < 2; h++) {      // the four columns of one half of the thread's
                 const u32x4 upper = transposed(u32x4{codes[0][h], codes[1][h], codes[2][h], codes[3][h]}), lower = transposed(u32x4{codes[4][h], codes[5][h], codes[6][h], codes[7][h]});
 #pragma unroll
-                for (int j = 0; j < 4; j++) *reinterpret_cast<u32x2 *>(turned + (8 * across + 4 * h + j) * PITCH + 8 * down) = u32x2{upper[j], lower[j]};
+                for (int j = 0; j < 4; j++) *reinterpret_cast<u32x2 *>(turned + ((h ? in_hi : in_lo) + j) * PITCH + 8 * down) = u32x2{upper[j], lower[j]};
             }
         }
         __syncthreads();

@@ -34,21 +34,26 @@ __device__ __forceinline__ void f8_round_rows(const F8Source &src, const F8Held 
             if constexpr (whole) x[i].load(at);
             else x[i].load_upto(at, row < src.rows ? count : 0);
         }
+        uint32_t amax = 0;      // of row lane mod 16 of the four: a scale's two divisions are some 25 instructions
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t found = most_of_16(bits_of(larger(larger(0, __builtin_convertvector(x[i].lo, f32x4)), __builtin_convertvector(x[i].hi, f32x4))));
+            amax = (lane & 15) == uint32_t(i) ? found : amax;
+        }
+        const float mine = f8_inverse(amax, most), inverses[4] = {of_lane_of_16<0>(mine), of_lane_of_16<1>(mine), of_lane_of_16<2>(mine), of_lane_of_16<3>(mine)};
+        if ((lane & 15) < 4) scales[lane >> 4][4 * wave + (lane & 15)] = f8_scale(amax, most);
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int64_t row = row0 + 4 * wave + i;
             const f32x4 lo = __builtin_convertvector(x[i].lo, f32x4), hi = __builtin_convertvector(x[i].hi, f32x4);
-            const uint32_t amax = most_of_16(bits_of(larger(larger(0, lo), hi)));
-            const float inverse = f8_inverse(amax, most);
             if ((whole || row < src.rows) && col < to.cols + (-to.cols & 127)) {      // behind the last element zeros: they were loaded as such, but NaN times zero is no zero
-                u32x2 codes{f8_codes(lo * inverse, to.e5m2), f8_codes(hi * inverse, to.e5m2)};
+                u32x2 codes{f8_codes(lo * inverses[i], to.e5m2), f8_codes(hi * inverses[i], to.e5m2)};
                 if (count < 8) {
-                    const uint64_t kept = (uint64_t(codes.y) << 32 | codes.x) & ((1ull << (8 * count)) - 1);
+                    const uint64_t kept = (uint64_t(codes.y) << 32 | codes.x) & ((1ull << (8 * (count & 7))) - 1);
                     codes = u32x2{uint32_t(kept), uint32_t(kept >> 32)};
                 }
                 __builtin_nontemporal_store(codes, (u32x2 DSLLM_GLOBAL *)(to.codes + row * to.code_pitch + col));
             }
-            if ((lane & 15) == 0) scales[lane >> 4][4 * wave + i] = f8_scale(amax, most);
         }
     };
     if (row0 + 16 <= src.rows && col0 + 512 <= src.cols) work(std::true_type{});

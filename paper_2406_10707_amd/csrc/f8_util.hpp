@@ -69,14 +69,17 @@ __device__ __forceinline__ float larger(float most, f32x4 v) {
     most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_fabsf(v[0]), __builtin_fabsf(v[1])), most);
     return __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_fabsf(v[2]), __builtin_fabsf(v[3])), most);
 }
-// Magnitudes' bits order like them, NaN above all.
-__device__ __forceinline__ uint32_t bits_of(float magnitude) { return __float_as_uint(magnitude) & 0x7FFFFFFFu; }
+// Magnitudes' bits order like them, NaN (whose sign is cleared as any other's) above all.
+__device__ __forceinline__ uint32_t bits_of(float magnitude) { return __float_as_uint(magnitude); }
 
 // The largest of sixteen neighbouring lanes' values (lanes 16 i to 16 i + 15), in all of them.
 __device__ __forceinline__ uint32_t most_of_16(uint32_t v) {
     v = most_of_8(v);
     return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x140, 0xF, 0xF, true)));      // the sixteen mirrored
 }
+// Lane I's value of each sixteen neighbouring lanes, in all of them.
+template <int I>
+__device__ __forceinline__ float of_lane_of_16(float v) { return __uint_as_float(uint32_t(__builtin_amdgcn_mov_dpp(int(__float_as_uint(v)), 0x150 + I, 0xF, 0xF, true))); }
 // The largest of lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them.
 __device__ __forceinline__ uint32_t most_of_quarters(uint32_t v) {
     v = max(v, uint32_t(__shfl_xor(int(v), 16)));

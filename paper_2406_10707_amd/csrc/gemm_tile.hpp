@@ -47,8 +47,8 @@ struct TileOrder {
     }
 };
 
-__device__ __forceinline__ GemmTile gemm_tile(const TileOrder &o) {
-    const uint32_t xcd = blockIdx.x & o.xcd_bits, tile = xcd * o.each + min(xcd, o.more) + (blockIdx.x >> o.xcd_shift);
+__device__ __forceinline__ GemmTile gemm_tile(const TileOrder &o, uint32_t block = blockIdx.x) {
+    const uint32_t xcd = block & o.xcd_bits, tile = xcd * o.each + min(xcd, o.more) + (block >> o.xcd_shift);
     const uint32_t s = TileOrder::divided(tile, o.per_strip, o.strip_inverse), in_s = tile - s * o.per_strip;
     const uint32_t rows_here = s < o.full_strips ? 8 : o.last_rows;
     const uint32_t col = TileOrder::divided(in_s, rows_here, s < o.full_strips ? 1u << 29 : o.last_inverse);
