@@ -41,8 +41,10 @@ inline double f8_cost(const F8Form &f, uint64_t m, uint64_t n, uint32_t steps, u
 inline uint64_t f8_part_pitch(uint64_t n) { return (n + 3) / 4 * 4; }
 inline uint64_t f8_part_bytes(uint64_t m, uint64_t n) { return m * f8_part_pitch(n) * 4; }
 
-// Up to sixteen rows of A have a kernel of their own: its waves for each 16 rows of B, 0 for other products.
-inline uint32_t f8_few_waves(uint64_t m, uint32_t steps) { return m > 16 ? 0 : steps <= 32 ? 2 : 4; }
+// Up to sixteen rows of A have a kernel of their own: its waves for each 16 rows of B. Two where K is up to 4096 and there is a block for every unit, else four: one row with 4096 x 4096 6.7 us (four 7.7), 1024 x 4096 4.2 (two 5.7),
+// 4096 x 11008 12.8 (two 14.1, eight 13.0), 28672 x 8192 42.0 (44.5, 43.9); of both halves of the gated block 11008 x 4096 21.1 (22.9), 28672 x 8192 82 (87).
+constexpr uint64_t kF8Few = 16;
+inline uint32_t f8_few_waves(uint64_t n, uint32_t steps) { return steps <= 32 && n >= 16 * kF8Units ? 2 : 4; }
 
 struct F8Choice { int form; uint32_t splits; };
 

@@ -134,13 +134,13 @@ __global__ __launch_bounds__(512, 2) void gated_forward_halves_kernel(GatedForwa
 // ------------------------------------------------------------------ up to sixteen tokens
 
 // Rows of `pitch` floats, sixteen a matrix: h, then gate and up
-template <int WAVES, int ACT, int FA>
+template <int WAVES, bool EIGHT, int ACT, int FA>
 __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(GatedForward p, float *values, uint64_t pitch) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[F8Few<WAVES, 2>::BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[F8Few<WAVES, 2, EIGHT>::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = int64_t(blockIdx.x) * 16;
     f32x4 sum[2];
-    F8Few<WAVES, 2>::template sums<FA, 0>(sum, p.x, p.w_gate, p.w_up, p.steps, n0, lds, lane, wave);
+    F8Few<WAVES, 2, EIGHT>::template sums<FA, 0>(sum, p.x, p.w_gate, p.w_up, p.steps, n0, lds, lane, wave);
     if (wave > 0 || (lane & 15) >= p.tokens) return;
     f32x4 h;
 #pragma unroll
@@ -360,13 +360,15 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
     const GatedForward p{f8_side(x), f8_side(w_gate), f8_side(w_up), F8Held(gate), F8Held(up), F8Held(h), tokens, ffn, steps};
     const bool x_e5m2 = x->format == CKPT_F8_E5M2;
     const int64_t across = (ffn + 127) / 128;
-    if (tokens <= 16 && steps && workspace && workspace_bytes >= few_bytes(ffn) && across < 1 << 20) {
+    if (uint64_t(tokens) <= kF8Few && steps && workspace && workspace_bytes >= few_bytes(ffn) && across < 1 << 20) {
         if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
         if (const char *why = ranges.wrong(workspace, few_bytes(ffn))) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
         float *values = static_cast<float *>(workspace);
         const uint64_t pitch = few_pitch(ffn);
         with_kinds(activation, x_e5m2, true, [&](auto act, auto fa, auto) {
-            hipLaunchKernelGGL((gated_few_kernel<4, act, fa>), dim3(unsigned((ffn + 15) / 16)), dim3(256), 0, stream, p, values, pitch);
+            auto launch = [&](auto waves, auto eight) { hipLaunchKernelGGL((gated_few_kernel<waves, eight, act, fa>), dim3(unsigned((ffn + 15) / 16)), dim3(64 * waves), 0, stream, p, values, pitch); };
+            if (f8_few_waves(uint64_t(ffn), steps) == 2) tokens <= 8 ? launch(std::integral_constant<int, 2>(), std::true_type()) : launch(std::integral_constant<int, 2>(), std::false_type());
+            else tokens <= 8 ? launch(std::integral_constant<int, 4>(), std::true_type()) : launch(std::integral_constant<int, 4>(), std::false_type());
         });
         hipLaunchKernelGGL(gated_round_kernel, dim3(unsigned((ffn + 511) / 512), gate ? 3 : 1), dim3(256), 0, stream, p, values, pitch);
         return launched();
@@ -451,7 +453,7 @@ int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *
         if (!bytes || tokens < 0 || ffn < 0 || hidden < 0) return refuse(CKPT_EINVAL, "null argument or negative size");
         *bytes = 0;
         if (tokens > 0x7FFFFFFF || ffn > 0x7FFFFFFF || hidden > kF8LongestRow) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1, or what is contracted over 2^23");
-        if (tokens && ffn && hidden && tokens <= 16) *bytes = few_bytes(ffn);
+        if (tokens && ffn && hidden && uint64_t(tokens) <= kF8Few) *bytes = few_bytes(ffn);
         return int(CKPT_OK);
     });
 }

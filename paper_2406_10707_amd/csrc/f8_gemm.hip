@@ -132,13 +132,13 @@ __device__ __forceinline__ void store_four(const F8Gemm &p, int64_t row, int64_t
     else store_four<CKPT_F16>(static_cast<_Float16 *>(p.c) + at, sum, count, p.accumulate);
 }
 
-template <int WAVES, int FA, int FB>
+template <int WAVES, bool EIGHT, int FA, int FB>
 __global__ __launch_bounds__(64 * WAVES) void f8_few_kernel(F8Gemm p) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[F8Few<WAVES, 1>::BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[F8Few<WAVES, 1, EIGHT>::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = int64_t(blockIdx.x) * 16;
     f32x4 sum[1];
-    F8Few<WAVES, 1>::template sums<FA, FB>(sum, p.a, p.b, p.b, p.steps, n0, lds, lane, wave);
+    F8Few<WAVES, 1, EIGHT>::template sums<FA, FB>(sum, p.a, p.b, p.b, p.steps, n0, lds, lane, wave);
     const int64_t col = n0 + 4 * (lane >> 4);
     if (wave == 0 && (lane & 15) < p.m && col < p.n) store_four(p, lane & 15, col, sum[0]);
 }
@@ -233,12 +233,14 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
     const uint32_t steps = f8_steps(uint64_t(k));
     F8Gemm p{f8_side(a), f8_side(b), c, ldc, m, n, steps, steps, 0, accumulate, dtype};
     const bool a_e5m2 = a->format == CKPT_F8_E5M2, b_e5m2 = b->format == CKPT_F8_E5M2, wide = dtype == CKPT_F32;
-    if (const uint32_t waves = f8_few_waves(uint64_t(m), steps)) {
+    if (uint64_t(m) <= kF8Few) {
+        const uint32_t waves = f8_few_waves(uint64_t(n), steps);
         launch_in_parts(p, 128, 16ll << 22, [&](const F8Gemm &part) {
             with_formats(a_e5m2, b_e5m2, [&](auto fa, auto fb) {
                 const dim3 grid(unsigned((part.n + 15) / 16));
-                if (waves == 2) hipLaunchKernelGGL((f8_few_kernel<2, fa, fb>), grid, dim3(128), 0, stream, part);
-                else hipLaunchKernelGGL((f8_few_kernel<4, fa, fb>), grid, dim3(256), 0, stream, part);
+                auto launch = [&](auto waves_, auto eight) { hipLaunchKernelGGL((f8_few_kernel<waves_, eight, fa, fb>), grid, dim3(64 * waves_), 0, stream, part); };
+                if (waves == 2) m <= 8 ? launch(std::integral_constant<int, 2>(), std::true_type()) : launch(std::integral_constant<int, 2>(), std::false_type());
+                else m <= 8 ? launch(std::integral_constant<int, 4>(), std::true_type()) : launch(std::integral_constant<int, 4>(), std::false_type());
             });
         });
         return launched();
@@ -273,7 +275,7 @@ int ckpt_f8_gemm_workspace(int64_t m, int64_t n, int64_t k, uint64_t *bytes) {
         if (!bytes || m < 0 || n < 0 || k < 0) return refuse(CKPT_EINVAL, "null argument or negative size");
         *bytes = 0;
         if (m > 0x7FFFFFFF || n > 0x7FFFFFFF || k > kF8LongestRow) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1, or what is contracted over 2^23");
-        if (!m || !n || !k || f8_few_waves(uint64_t(m), f8_steps(uint64_t(k)))) return int(CKPT_OK);
+        if (!n || !k || uint64_t(m) <= kF8Few) return int(CKPT_OK);
         for (int kind = 0; kind < 4; kind++) {
             const F8Choice c = f8_choice(uint64_t(m), uint64_t(n), uint64_t(k), kind & 1, kind >> 1, UINT64_MAX);
             if (c.splits > 1) *bytes = std::max(*bytes, f8_part_bytes(uint64_t(m), uint64_t(n)) * c.splits);

@@ -99,12 +99,12 @@ struct F8Loader {
     }
 };
 
-// What a wave of a product of up to sixteen rows of A loads: 16 rows of A and of each of MATRICES, 128 bytes a row and step, four steps to a window. LDS of a wave: the places of four steps, of each A's 16, then the others'; then two windows'
+// What a wave of a product of up to sixteen rows of A (EIGHT: up to eight) loads: 16 (8) rows of A and 16 of each of MATRICES, 128 bytes a row and step, four steps to a window. LDS of a wave: the places of four steps, of each A's, then the others'; then two windows'
 // scales, for each step 16 of A and 16 of each matrix. Rows past the end are the last row again; pieces of a place are permuted as in the tiles.
-template <int MATRICES>
+template <int MATRICES, bool EIGHT>
 struct F8FewLoader {
-    static constexpr int SIDES = 1 + MATRICES, STEP = SIDES * 2048, SCALES = 4 * SIDES * 64, STEP_LOADS = 2 * SIDES, SCALE_LOADS = SIDES, WAVE = 4 * STEP + 2 * SCALES;
-    const uint8_t *from[STEP_LOADS];      // this lane's piece of the rows lane / 8 and that + 8 of each side
+    static constexpr int SIDES = 1 + MATRICES, A_PLACES = EIGHT ? 1024 : 2048, STEP = A_PLACES + MATRICES * 2048, SCALES = 4 * SIDES * 64, STEP_LOADS = STEP / 1024, SCALE_LOADS = SIDES, WAVE = 4 * STEP + 2 * SCALES;
+    const uint8_t *from[STEP_LOADS];      // this lane's piece of the rows lane / 8 and, if there are so many, that + 8 of each side
     const float *scale_from[SCALE_LOADS];
     uint32_t scale_step[SCALE_LOADS], steps;
     uint64_t scale_pitch[SCALE_LOADS];
@@ -112,9 +112,10 @@ struct F8FewLoader {
     __device__ __forceinline__ F8FewLoader(const F8Side &a, const F8Side &b, const F8Side &b2, uint32_t steps_, int64_t n0, int lane) : steps(steps_) {
 #pragma unroll
         for (int i = 0; i < STEP_LOADS; i++) {
-            const int r = 8 * (i & 1) + (lane >> 3);
-            const F8Side &side = i < 2 ? a : i < 4 ? b : b2;
-            from[i] = side.codes + min((i < 2 ? 0 : n0) + r, side.rows - 1) * side.pitch + 16 * ((lane & 7) ^ f8_rotated((r >> 1) & 7));
+            constexpr int OF_A = A_PLACES / 1024;
+            const int r = 8 * (i < OF_A ? i : (i - OF_A) & 1) + (lane >> 3);
+            const F8Side &side = i < OF_A ? a : i < OF_A + 2 ? b : b2;
+            from[i] = side.codes + min((i < OF_A ? 0 : n0) + r, side.rows - 1) * side.pitch + 16 * ((lane & 7) ^ f8_rotated((r >> 1) & 7));
         }
 #pragma unroll
         for (int i = 0; i < SCALE_LOADS; i++) {      // scale 64 i + lane of a window: step, then side, then row

@@ -290,9 +290,9 @@ __device__ __forceinline__ void f8_sums(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds
 
 // As single tokens give them: B is what has to be read, once, at the rate of memory. A block takes 16 rows of B (of each of MATRICES); its waves take the windows of four steps in turn, each with LDS of its own, so that none waits
 // for another before the sums are added, in wave order. Four steps of B and A are under way a wave; a step's place is filled again as soon as it has been read.
-template <int WAVES, int MATRICES>
+template <int WAVES, int MATRICES, bool EIGHT>
 struct F8Few {
-    typedef F8FewLoader<MATRICES> Loader;
+    typedef F8FewLoader<MATRICES, EIGHT> Loader;
     static constexpr int SIDES = Loader::SIDES, STEP = Loader::STEP, BYTES = WAVES * Loader::WAVE;
 
     // sum[x] of wave 0: of row ar = lane mod 16 of A with the rows n0 + 4 (lane / 16) to that + 3 of matrix x
@@ -301,7 +301,13 @@ struct F8Few {
         const int q = lane >> 4, ar = lane & 15;
         uint8_t *mine = lds + wave * Loader::WAVE;
         const Loader load(a, b, b2, steps, n0, lane);
-        const int swizzle = f8_rotated((ar >> 1) & 7), x0 = ar * 128 + 16 * ((2 * q) ^ swizzle), x1 = ar * 128 + 16 * ((2 * q + 1) ^ swizzle);
+        int xa[2], xb[2];      // with eight rows of A lanes 8 to 15 take them again
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int place = EIGHT ? ar & 7 : ar;
+            xa[h] = place * 128 + 16 * ((2 * q + h) ^ f8_rotated((place >> 1) & 7));
+            xb[h] = ar * 128 + 16 * ((2 * q + h) ^ f8_rotated((ar >> 1) & 7));
+        }
         const uint32_t windows = (steps + 3) / 4;
 #pragma unroll
         for (int x = 0; x < MATRICES; x++) sum[x] = f32x4{0, 0, 0, 0};
@@ -314,8 +320,9 @@ struct F8Few {
                 u32x4 lo[SIDES], hi[SIDES];
 #pragma unroll
                 for (int i = 0; i < SIDES; i++) {
-                    lo[i] = *reinterpret_cast<const u32x4 *>(mine + s * STEP + 2048 * i + x0);
-                    hi[i] = *reinterpret_cast<const u32x4 *>(mine + s * STEP + 2048 * i + x1);
+                    const uint8_t *at = mine + s * STEP + (i ? Loader::A_PLACES + 2048 * (i - 1) : 0);
+                    lo[i] = *reinterpret_cast<const u32x4 *>(at + (i ? xb[0] : xa[0]));
+                    hi[i] = *reinterpret_cast<const u32x4 *>(at + (i ? xb[1] : xa[1]));
                 }
                 const float *scales = reinterpret_cast<const float *>(mine + 4 * STEP + (odd & 1) * Loader::SCALES) + 16 * SIDES * s;
                 float sa = scales[ar];

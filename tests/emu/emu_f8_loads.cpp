@@ -136,10 +136,10 @@ void tiles(const char *name) {
     tile<S>(a, b, b2, 1 << 16, 256 / S::BM * S::BM, 256);
 }
 
-template <int MATRICES>
+template <int MATRICES, bool EIGHT>
 void few() {
-    typedef F8FewLoader<MATRICES> L;
-    for (uint64_t m : {1, 2, 7, 16})
+    typedef F8FewLoader<MATRICES, EIGHT> L;
+    for (uint64_t m : {1, 2, 7, EIGHT ? 8 : 16})
         for (uint64_t n : {1, 5, 16, 17, 300})
             for (uint64_t k : {1, 128, 129, 512, 1300, 5000})
                 for (uint32_t shift : {0, 7}) {
@@ -163,10 +163,11 @@ void few() {
                             for (uint32_t s = 0; s < 4 && 4 * window + s < steps; s++)
                                 for (int x = 0; x < L::SIDES; x++)
                                     for (int r = 0; r < 16; r++) {
+                                        const bool held = x || !EIGHT || r < 8;
                                         const F8Side &of = x == 0 ? a : x == 1 ? b : b2;
                                         const int64_t row = (x ? n0 : 0) + r;
                                         for (int piece = 0; piece < 8; piece++)
-                                            if (landed[s * L::STEP + 2048 * x + 128 * r + 16 * (piece ^ f8_rotated((r >> 1) & 7))] != code_at(of, row, 4 * window + s, piece)) fail("codes");
+                                            if (held && landed[s * L::STEP + (x ? L::A_PLACES + 2048 * (x - 1) : 0) + 128 * r + 16 * (piece ^ f8_rotated((r >> 1) & 7))] != code_at(of, row, 4 * window + s, piece)) fail("codes");
                                         if (landed[4 * L::STEP + (window & 1) * L::SCALES + 4 * (16 * L::SIDES * s + 16 * x + r)] != scale_at(of, row, 4 * window + s)) fail("scales");
                                     }
                         }
@@ -182,7 +183,9 @@ int main() {
     tiles<F8Shape<4, 2, 4, 8, 4, 2, true>>("pair 256x256");
     tiles<F8Shape<4, 2, 2, 8, 4, 2, true>>("pair 128x256");
     tiles<F8Shape<2, 4, 2, 4, 2, 2, true>>("pair 64x256");
-    few<1>();
-    few<2>();
+    few<1, false>();
+    few<1, true>();
+    few<2, false>();
+    few<2, true>();
     printf("ok %llu loads\n", count);
 }
