@@ -4,7 +4,7 @@
 
 namespace dsllm {
 
-// A form's tile, how many of its blocks share a compute unit, and what it costs, about microseconds, fitted to 1200 times of 26 products from 300 x 2050 x 768 to 11008 x 4096 x 8192: a step of 128 values of K with blocks on every unit (and in
+// A form's tile, how many of its blocks share a compute unit, and what it costs, about microseconds, fitted to 1500 times of 32 products from 300 x 2050 x 768 to 8192^3: a step of 128 values of K with blocks on every unit (and in
 // every round but the last) or, of forms whose blocks share a unit, with one on it; what a block takes besides, with C in 16 bits or in f32. Steps for the two kinds of sums (8-bit instructions, bf16) and of B's scales (of 128 x 128,
 // of single rows). The choice is in the mean 1 % over the best
 // form, at most 8 %.
@@ -17,14 +17,14 @@ struct F8Form {
 // Sums of the 8-bit instructions with scales of single rows do not fit the registers of a 64 x 128 wave (they spill: 8192^3 650 us, with 256 x 128 tiles 555).
 constexpr double kF8Never = 1e9;
 constexpr F8Form kF8Forms[] = {
-    {"256x256", 256, 256, 1, {{0.99, 1.59}, {kF8Never, kF8Never}, {2.49, 3.36}, {3.20, 3.90}}, {8.9, 9.0}},
-    {"256x128", 256, 128, 1, {{0.64, 0.88}, {0.84, 1.07}, {1.49, 1.74}, {1.75, 1.92}}, {5.1, 5.0}},
-    {"128x128", 128, 128, 2, {{0.58, 0.94}, {0.65, 1.06}, {1.04, 1.69}, {1.22, 1.87}}, {3.6, 3.3}},
-    {"64x64", 64, 64, 2, {{0.22, 0.36}, {0.27, 0.41}, {0.47, 0.63}, {0.53, 0.71}}, {2.8, 2.5}},
+    {"256x256", 256, 256, 1, {{1.13, 1.56}, {kF8Never, kF8Never}, {2.93, 3.34}, {3.26, 3.63}}, {8.9, 9.8}},
+    {"256x128", 256, 128, 1, {{0.63, 0.89}, {0.84, 1.09}, {1.47, 1.69}, {1.65, 1.87}}, {5.7, 6.2}},
+    {"128x128", 128, 128, 2, {{0.57, 0.96}, {0.63, 1.08}, {1.00, 1.69}, {1.19, 1.86}}, {4.1, 3.9}},
+    {"64x64", 64, 64, 2, {{0.22, 0.38}, {0.27, 0.41}, {0.47, 0.65}, {0.52, 0.73}}, {2.8, 2.5}},
 };
 constexpr int kF8FormCount = sizeof(kF8Forms) / sizeof(kF8Forms[0]);
 constexpr uint32_t kF8Units = 256;
-constexpr double kF8Join = 3.0, kF8JoinSplit = 0.45, kF8JoinBytes = 10.5e6;      // what joining parts of K costs besides, for each part, bytes a unit of cost
+constexpr double kF8Join = 3.0, kF8JoinSplit = 0.45, kF8JoinBytes = 11.9e6;      // what joining parts of K costs besides, for each part, bytes a unit of cost
 constexpr uint64_t kF8MostTiles = 1u << 22;              // of a launch
 
 inline uint32_t f8_steps(uint64_t k) { return uint32_t((k + 127) / 128); }
@@ -64,10 +64,21 @@ inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool wide, bool ro
     return best;
 }
 
-// The gated block's forward pass: tiles of 256, 128 or 64 tokens by 128 columns of gate and of up.
-inline int gated_form(uint64_t tokens, uint64_t across) {
-    if ((tokens + 255) / 256 * across >= kF8Units) return 0;
-    return (tokens + 127) / 128 * across >= kF8Units ? 1 : 2;
+// The gated block's forward pass: tiles of 256, 128 or 64 tokens by 128 columns of gate and of up, a block a unit, or (kGatedHalves) of 256 with the last round's in halves. By what a round of them costs, about microseconds: 4096 to 11008 columns
+// 64 tokens 38 us (60 by tiles of 128, 99 of 256), 256 tokens 65 (78 by 64, 98 by 256), 512 tokens 104 (122, 116), 1024 tokens 163 with halves (204 without, 185 by 128).
+constexpr int kGatedHalves = 3;
+inline int gated_form(uint64_t tokens, uint64_t across, uint32_t steps) {
+    constexpr uint64_t rows[] = {256, 128, 64};
+    constexpr double step[] = {2.75, 1.62, 0.97}, block[] = {10.6, 7.7, 6.9};
+    auto round = [&](int f) { return step[f] * steps + block[f]; };
+    int best = 0;
+    double least = 0;
+    for (int f = 0; f < 3; f++) {
+        const double t = double(((tokens + rows[f] - 1) / rows[f] * across + kF8Units - 1) / kF8Units) * round(f);
+        if (f == 0 || t < least) { best = f; least = t; }
+    }
+    const uint64_t count = (tokens + 255) / 256 * across, rest = count % kF8Units;
+    return count > kF8Units && rest && 2 * rest <= kF8Units && double(count / kF8Units) * round(0) + round(1) < least ? kGatedHalves : best;
 }
 
 }  // namespace dsllm

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForwa
     gated_forward_tile<S, ACT, SQUARE, FA>(p, lds, int64_t(t.tm) * S::BM, int64_t(t.tn) * 128);
 }
 
-// Tiles of 256 tokens up to the `whole`th block; behind them each two blocks take the halves of one, where the last round of blocks would leave half of the chip idle: 4096 tokens, 4096 to 11008, 5.4 rounds, 629 -> 603 us.
+// Tiles of 256 tokens up to the `whole`th block; behind them each two blocks take the halves of one, where the last round of blocks would leave half of the chip idle: 4096 tokens, 4096 to 11008, 5.4 rounds, 601 -> 569 us; 1024 tokens 204 -> 163.
 template <int ACT, bool SQUARE, int FA>
 __global__ __launch_bounds__(512, 2) void gated_forward_halves_kernel(GatedForward p, TileOrder order, uint32_t whole) {
     typedef F8Shape<4, 2, 4, 8, 4, 2, true> S;
@@ -316,6 +316,7 @@ void with_kinds(int32_t activation, bool e5m2, bool square, F f) {
 
 // Sides are at most 2^31 - 1; the product of tiles is at most 2^24 - 1, so that a grid has fewer than 2^32 work-items.
 bool fits_grid(int64_t down, int64_t across) { return down * across < 1 << 22; }
+constexpr const char *kTooManyTiles = "more than 2^22 tiles of tokens and columns";
 
 bool overlap(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b) {
     if (!a || !b || !a->rows || !a->cols || !b->rows || !b->cols) return false;
@@ -376,21 +377,22 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
     auto tiles = [&](auto shape) {
         typedef decltype(shape) S;
         const int64_t down = (tokens + S::BM - 1) / S::BM;
-        if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, "more than 2^22 tiles of tokens and columns");
+        if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooManyTiles);
         const dim3 grid(unsigned(down * across)), block(S::THREADS);
         const TileOrder order(uint32_t(down), uint32_t(across), true);
         with_kinds(activation, x_e5m2, p.w_gate.shift, [&](auto act, auto fa, auto square) { hipLaunchKernelGGL((gated_forward_kernel<S, act, square, fa>), grid, block, 0, stream, p, order); });
         return launched();
     };
-    switch (gated_form(uint64_t(tokens), uint64_t(across))) {
-        case 0: {
+    switch (gated_form(uint64_t(tokens), uint64_t(across), steps)) {
+        case kGatedHalves: {
             const int64_t down = (tokens + 255) / 256, count = down * across, rest = count % kF8Units;
-            if (!fits_grid(down, across) || rest == 0 || 2 * rest > kF8Units) return tiles(F8Shape<4, 2, 4, 8, 4, 2, true>());
+            if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooManyTiles);
             with_kinds(activation, x_e5m2, p.w_gate.shift, [&](auto act, auto fa, auto square) {
                 hipLaunchKernelGGL((gated_forward_halves_kernel<act, square, fa>), dim3(unsigned(count + rest)), dim3(512), 0, stream, p, TileOrder(uint32_t(down), uint32_t(across), true), uint32_t(count - rest));
             });
             return launched();
         }
+        case 0: return tiles(F8Shape<4, 2, 4, 8, 4, 2, true>());
         case 1: return tiles(F8Shape<4, 2, 2, 8, 4, 2, true>());
         default: return tiles(F8Shape<2, 4, 2, 4, 2, 2, true>());
     }
@@ -434,7 +436,7 @@ int backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down, const ckpt_
     const GatedBackward p{f8_side(dy), f8_side(w_down), F8Held(gate), F8Held(up), F8Held(grads->dgate), F8Held(grads->dup), F8Held(grads->dgate_by_col), F8Held(grads->dup_by_col), F8Held(grads->h_by_col),
                           tokens, ffn, f8_steps(uint64_t(dy->cols))};
     const int64_t down = (tokens + 127) / 128, across = (ffn + 127) / 128;
-    if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, "more than 2^22 tiles of tokens and columns");
+    if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooManyTiles);
     const dim3 grid(unsigned(down * across));
     const TileOrder order(uint32_t(down), uint32_t(across), true);
     with_kinds(activation, dy->format == CKPT_F8_E5M2, p.w_down.shift, [&](auto act, auto fa, auto square) {
