@@ -143,7 +143,7 @@ int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *
 int ckpt_gated_forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8_matrix *w_up, int32_t activation, const ckpt_f8_matrix *gate,
                        const ckpt_f8_matrix *up, const ckpt_f8_matrix *h, void *workspace, uint64_t workspace_bytes, void *stream);
 
-/* What ckpt_gated_backward writes, each or NULL, all with block_rows 1, gradients in either format (one for all), h as CKPT_F8_E4M3: by rows (tokens x ffn) for dx = dgate Wg + dup Wu, by columns (ffn x tokens) for the weights' gradients. */
+/* What ckpt_gated_backward writes, each or NULL, all with block_rows 1, gradients in either format (one for all), h as CKPT_F8_E4M3: by rows (tokens x ffn) for dx = dgate Wg + dup Wu, by columns (ffn x tokens, a pitch of at most 2^23) for the weights' gradients. */
 typedef struct {
     const ckpt_f8_matrix *dgate, *dup, *dgate_by_col, *dup_by_col, *h_by_col;
 } ckpt_gated_grads;

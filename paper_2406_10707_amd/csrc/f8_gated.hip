@@ -14,19 +14,19 @@ namespace {
 
 // act(g) = g s with s = 1 / (1 + exp(-z)): z is g for SiLU, 2 sqrt(2 / pi) (g + 0.044715 g^3) for GELU (its tanh(x) is 2 / (1 + exp(-2 x)) - 1).
 constexpr float kGelu = 1.5957691216057308f, kCubic = 0.044715f;
-// exp(-z)
 template <int ACT>
-__device__ __forceinline__ float exp_of(float g) {
+__device__ __forceinline__ float sigmoid_of(float g) {
     const float z = ACT == CKPT_GATE_SILU ? g : kGelu * g * __builtin_fmaf(kCubic * g, g, 1.0f);
-    return __builtin_amdgcn_exp2f(-1.4426950408889634f * z);
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
 }
-__device__ __forceinline__ float sigmoid_of(float e) { return __builtin_amdgcn_rcpf(1.0f + e); }
-// act'(g) = s + act(g) (1 - s) dz/dg. 1 - s is e s, without cancellation; where e is infinite that is NaN, and the smaller of it and 1 is 1. Where the factors of dz/dg are zero it may be infinite.
+// act'(g) = s + act(g) (1 - s) dz/dg. 1 - s is off by up to 2^-23 where s nears 1; act(g) dz/dg is below 40 there (for larger g, s is 1 and the second term below 2^-18 left out): 5e-6 of the slope, where a code's half step is 2^-4. Where act(g) (1 - s) is zero dz/dg may be infinite.
 template <int ACT>
-__device__ __forceinline__ float slope_of(float g, float e, float s, float act) {
-    const float t = act * fminf(e * s, 1.0f);
-    if constexpr (ACT == CKPT_GATE_SILU) return s + t;
-    else return t == 0 ? s : __builtin_fmaf(t, kGelu * __builtin_fmaf(3 * kCubic * g, g, 1.0f), s);
+__device__ __forceinline__ float slope_of(float g, float s, float act) {
+    if constexpr (ACT == CKPT_GATE_SILU) return __builtin_fmaf(act, 1.0f - s, s);
+    else {
+        const float t = act * (1.0f - s);
+        return t == 0 ? s : __builtin_fmaf(t, kGelu * __builtin_fmaf(3 * kCubic * g, g, 1.0f), s);
+    }
 }
 
 // Which bytes of a word of four codes stay where `left` columns are left.
@@ -65,7 +65,7 @@ __device__ __forceinline__ void gated_forward_tile(const GatedForward &p, uint8_
         for (int j = 0; j < S::TNG; j++) {
             const f32x4 g = acc[i][j], u = acc[i][S::TNG + j];
 #pragma unroll
-            for (int e = 0; e < 4; e++) h[i][j][e] = g[e] * sigmoid_of(exp_of<ACT>(g[e])) * u[e];
+            for (int e = 0; e < 4; e++) h[i][j][e] = g[e] * sigmoid_of<ACT>(g[e]) * u[e];
             most_h = larger(most_h, h[i][j]);
             most_gate = larger(most_gate, g);
             most_up = larger(most_up, u);
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(GatedForward p, f
     if (wave > 0 || (lane & 15) >= p.tokens) return;
     f32x4 h;
 #pragma unroll
-    for (int e = 0; e < 4; e++) h[e] = sum[0][e] * sigmoid_of(exp_of<ACT>(sum[0][e])) * sum[1][e];
+    for (int e = 0; e < 4; e++) h[e] = sum[0][e] * sigmoid_of<ACT>(sum[0][e]) * sum[1][e];
     float *at = values + (lane & 15) * pitch + n0 + 4 * (lane >> 4);
     *(f32x4 DSLLM_GLOBAL *)at = h;
     if (!p.gate.codes) return;
@@ -216,8 +216,8 @@ __global__ __launch_bounds__(256, 2) void gated_backward_kernel(GatedBackward p,
             const f32x4 g = fp8_values(parked[(8 * j + i) * 256 + threadIdx.x]) * gate_scale[i], u = fp8_values(parked[(8 * j + 4 + i) * 256 + threadIdx.x]) * up_scale[i];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                const float ex = exp_of<ACT>(g[e]), s = sigmoid_of(ex), act = g[e] * s, dh = dgate[i][j][e];
-                dgate[i][j][e] = dh * u[e] * slope_of<ACT>(g[e], ex, s, act);
+                const float s = sigmoid_of<ACT>(g[e]), act = g[e] * s, dh = dgate[i][j][e];
+                dgate[i][j][e] = dh * u[e] * slope_of<ACT>(g[e], s, act);
                 dup[i][j][e] = dh * act;
                 h[i][j][e] = act * u[e];
             }
@@ -227,16 +227,17 @@ __global__ __launch_bounds__(256, 2) void gated_backward_kernel(GatedBackward p,
             most_dup[i] = larger(most_dup[i], dup[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        uint32_t found[12];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            auto column = [&](uint32_t &of, const f32x4 (&v)[4][4]) {
-                const uint32_t found = most_of_16(bits_of(larger(0, f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]})));
-                of = ar == 4 * j + e ? found : of;
-            };
-            column(of_column[0], dgate);
-            column(of_column[1], dup);
-            column(of_column[2], h);
+            auto column = [&](const f32x4 (&v)[4][4]) { return bits_of(larger(0, f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]})); };
+            found[3 * e] = column(dgate);
+            found[3 * e + 1] = column(dup);
+            found[3 * e + 2] = column(h);
         }
+        most_of_16(found);
+#pragma unroll
+        for (int k = 0; k < 12; k++) of_column[k % 3] = ar == 4 * j + k / 3 ? found[k] : of_column[k % 3];
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -278,16 +279,21 @@ __global__ __launch_bounds__(256, 2) void gated_backward_kernel(GatedBackward p,
         }
     };
     const uint32_t rows_kept = bytes_kept(p.tokens - my_row);
+    // a column past the end lies past the descriptor's end, and is not stored
+    const uint32_t columns = uint32_t(min(p.ffn - col, int64_t(128)));
     auto by_col = [&](const F8Held &to, int first, const f32x4 (&v)[4][4], bool e5m2) {
         if (!to.codes) return;
-        uint8_t *at = to.codes + my_col * to.code_pitch + my_row;
+        const uint32_t pitch = uint32_t(to.code_pitch);
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(to.codes + col * to.code_pitch + row, 0, (columns - 1) * pitch + 128, 0x00020000);
+        uint32_t at = (64 * wn + 16 * q) * pitch + uint32_t(my_row - row);
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const f32x4 inverse = *reinterpret_cast<const f32x4 *>(inverses + first + 64 * wn + 16 * q + 4 * j);
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (my_col + 4 * j + e < p.ffn)
-                    *(uint32_t DSLLM_GLOBAL *)(at + (4 * j + e) * to.code_pitch) = f8_codes(f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]} * inverse[e], e5m2) & rows_kept;
+            for (int e = 0; e < 4; e++) {
+                __builtin_amdgcn_raw_buffer_store_b32(f8_codes(f32x4{v[0][j][e], v[1][j][e], v[2][j][e], v[3][j][e]} * inverse[e], e5m2) & rows_kept, rsrc, at, 0, 0);
+                at += pitch;
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -415,6 +421,8 @@ int backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down, const ckpt_
         if (const char *why = wrong_f8_contraction(every[i].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + why);
     if (w_down->format != CKPT_F8_E4M3) return refuse(CKPT_EINVAL, "w_down_by_col must be CKPT_F8_E4M3");
     int32_t format = 0;
+    for (int i = 6; i < 9; i++)
+        if (every[i].m && every[i].m->code_pitch > uint64_t(kF8LongestRow)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "a pitch of at most 2^23 is wanted");
     for (int i = 4; i < 8; i++)
         if (every[i].m) {
             if (format && every[i].m->format != format) return refuse(CKPT_EINVAL, "the gradients differ in their format");

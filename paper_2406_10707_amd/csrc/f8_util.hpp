@@ -46,14 +46,15 @@ __device__ __forceinline__ float f8_scale(uint32_t amax_bits, float most) {
     if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
     return fmaxf(__uint_as_float(amax_bits) / most, 0x1p-126f);
 }
-// Codes of four values of at most the format's largest, element 0 lowest. The conversions round to nearest, ties to even.
+// Codes of four values of at most the format's largest, element 0 lowest. The conversions round to nearest, ties to even. Each writes half of a word and leaves the other half: what is there before the first does not matter, and a value
+// that is not needed any more is no instruction.
 __device__ __forceinline__ uint32_t f8_codes(f32x4 y, bool e5m2) {
-    int r;
+    int r = int(__float_as_uint(y[0]));
     if (e5m2) {
-        r = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], 0, false);
+        r = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], r, false);
         r = __builtin_amdgcn_cvt_pk_bf8_f32(y[2], y[3], r, true);
     } else {
-        r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], r, false);
         r = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
     }
     return uint32_t(r);
@@ -77,6 +78,19 @@ __device__ __forceinline__ uint32_t most_of_16(uint32_t v) {
     v = most_of_8(v);
     return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x140, 0xF, 0xF, true)));      // the sixteen mirrored
 }
+// The same of several values at a time: between an instruction and one that takes its result from another lane stand those of the other values instead of waits.
+template <int N>
+__device__ __forceinline__ void most_of_16(uint32_t (&v)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; k++) v[k] = max(v[k], uint32_t(__builtin_amdgcn_mov_dpp(int(v[k]), 0xB1, 0xF, 0xF, true)));
+#pragma unroll
+    for (int k = 0; k < N; k++) v[k] = max(v[k], uint32_t(__builtin_amdgcn_mov_dpp(int(v[k]), 0x4E, 0xF, 0xF, true)));
+#pragma unroll
+    for (int k = 0; k < N; k++) v[k] = max(v[k], uint32_t(__builtin_amdgcn_mov_dpp(int(v[k]), 0x141, 0xF, 0xF, true)));
+#pragma unroll
+    for (int k = 0; k < N; k++) v[k] = max(v[k], uint32_t(__builtin_amdgcn_mov_dpp(int(v[k]), 0x140, 0xF, 0xF, true)));
+}
+
 // Lane I's value of each sixteen neighbouring lanes, in all of them.
 template <int I>
 __device__ __forceinline__ float of_lane_of_16(float v) { return __uint_as_float(uint32_t(__builtin_amdgcn_mov_dpp(int(__float_as_uint(v)), 0x150 + I, 0xF, 0xF, true))); }

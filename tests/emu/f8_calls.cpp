@@ -199,6 +199,10 @@ void refusals() {
     REFUSED(backward(&dy, &wd, &gate, &up, CKPT_GATE_SILU, {&dgate, &dgate}));
     REFUSED(backward(&dy, &wd, &gate, &up, CKPT_GATE_SILU, {&gate}));                  // in the place of what is read
     REFUSED(backward(&dy, &ws2, &gate, &up, CKPT_GATE_SILU, {&dgate}));
+    auto pitched = [&](uint64_t pitch) { return but(dgc, [&](auto &x) { x.code_pitch = pitch; x.codes = allocate(300 * pitch); }); };
+    const auto longest = pitched(1 << 23), longer = pitched((1 << 23) + 16);
+    TAKEN(backward(&dy, &wd, &gate, &up, CKPT_GATE_SILU, {nullptr, nullptr, &longest}));
+    REFUSED(backward(&dy, &wd, &gate, &up, CKPT_GATE_SILU, {nullptr, nullptr, &longer}));
     malformed(dy, [&](const ckpt_f8_matrix *m) { return backward(m, &wd, &gate, &up, CKPT_GATE_SILU, {&dgate}); });
     malformed(gate, [&](const ckpt_f8_matrix *m) { return backward(&dy, &wd, m, &up, CKPT_GATE_SILU, {&dgate}); });
     malformed(dgc, [&](const ckpt_f8_matrix *m) { return backward(&dy, &wd, &gate, &up, CKPT_GATE_SILU, {nullptr, nullptr, m}); });
