@@ -163,6 +163,8 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
         });
     }
     if constexpr (BY_COL) {
+        // a column's pieces of 16 bytes are rotated by one for each 16 columns: a wave's lanes, whose columns are 8 (4) apart, write to all banks
+        auto place = [&](uint32_t c) { return reinterpret_cast<u32x2 *>(turned + c * PITCH + (16 * (c >> 4) + 8 * down) % 128); };
         if constexpr (!SQUARE) {
             uint32_t most[8];      // bits of magnitudes, which order like them
 #pragma unroll
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
             for (int j = 0; j < 8; j++) {
                 auto at = [&](int i) { return j < 4 ? lo[i][j & 3] : hi[i][j & 3]; };
                 const float by = j < 4 ? by_lo[j & 3] : by_hi[j & 3];
-                *reinterpret_cast<u32x2 *>(turned + ((j < 4 ? in_lo : in_hi) + (j & 3)) * PITCH + 8 * down) =
+                *place((j < 4 ? in_lo : in_hi) + (j & 3)) =
                     u32x2{f8_codes(f32x4{at(0), at(1), at(2), at(3)} * by, by_col.e5m2) & upper, f8_codes(f32x4{at(4), at(5), at(6), at(7)} * by, by_col.e5m2) & lower};
             }
         } else {
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
             for (int h = 0; h < 2; h++) {      // the four columns of one half of the thread's
                 const u32x4 upper = transposed(u32x4{codes[0][h], codes[1][h], codes[2][h], codes[3][h]}), lower = transposed(u32x4{codes[4][h], codes[5][h], codes[6][h], codes[7][h]});
 #pragma unroll
-                for (int j = 0; j < 4; j++) *reinterpret_cast<u32x2 *>(turned + ((h ? in_hi : in_lo) + j) * PITCH + 8 * down) = u32x2{upper[j], lower[j]};
+                for (int j = 0; j < 4; j++) *place((h ? in_hi : in_lo) + j) = u32x2{upper[j], lower[j]};
             }
         }
         __syncthreads();
@@ -203,7 +205,7 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(F8Source src, F8Held by_ro
         for (int i = 0; i < 4; i++) {
             const uint32_t c = 32 * i + (threadIdx.x >> 3), piece = 16 * (threadIdx.x & 7);
             if (whole || col0 + c < src.cols)
-                __builtin_nontemporal_store(*reinterpret_cast<const u32x4 *>(turned + c * PITCH + piece), (u32x4 DSLLM_GLOBAL *)(by_col.codes + (col0 + c) * by_col.code_pitch + 128 * uint64_t(tile_down) + piece));
+                __builtin_nontemporal_store(*reinterpret_cast<const u32x4 *>(turned + c * PITCH + (16 * (c >> 4) + piece) % 128), (u32x4 DSLLM_GLOBAL *)(by_col.codes + (col0 + c) * by_col.code_pitch + 128 * uint64_t(tile_down) + piece));
         }
     }
 }
