@@ -56,7 +56,7 @@ inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool wide, bool ro
     for (int f = 0; f < kF8FormCount; f++)
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
             const uint32_t each = (steps + splits - 1) / splits;
-            if (splits > 1 && (uint64_t(each) * (splits - 1) >= steps || f8_part_bytes(m, n) > workspace / splits || kF8Forms[f].tiles(m, n) > kF8MostTiles)) break;
+            if (splits > 1 && (uint64_t(each) * (splits - 1) >= steps || f8_part_bytes(m, n) > workspace / splits || kF8Forms[f].tiles(m, n) > kF8MostTiles || m * f8_part_pitch(n) >> 33)) break;      // one launch for the tiles, one of 2^31 threads at most that joins them
             double t = f8_cost(kF8Forms[f], m, n, each, splits, wide, rows);
             if (splits > 1) t += kF8Join + kF8JoinSplit * splits + double(f8_part_bytes(m, n)) * (2 * splits + 1) / kF8JoinBytes;
             if ((f == 0 && splits == 1) || t < least) { best = F8Choice{f, splits}; least = t; }
