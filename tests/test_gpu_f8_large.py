@@ -16,10 +16,11 @@ ONE = int(fo.nearest_codes(np.ones(1), fo.E4M3)[0])
 class Large:
     """rows x cols, all codes `byte`, all scales `scale`."""
 
-    def __init__(self, rows, cols, byte=0, scale=1.0, fmt=fo.E4M3, block_rows=1):
+    def __init__(self, rows, cols, byte=0, scale=1.0, fmt=fo.E4M3, block_rows=1, pitch=None):
         self.rows, self.cols, self.fmt = rows, cols, fmt
         self.pitch, self.scale_pitch = B.f8_layout(fmt, rows, cols, block_rows)
-        self.codes, self.scales = harness.DevBuf(rows * self.pitch), harness.DevBuf(4 * self.pitch // 128 * self.scale_pitch)
+        self.pitch = pitch or self.pitch
+        self.codes, self.scales = harness.DevBuf(rows * self.pitch), harness.DevBuf(4 * (fo.padded(cols) // 128) * self.scale_pitch)
         B.proxy_device_fill_async(self.codes.ptr, byte, self.codes.nbytes, 0)
         ones = np.full(self.scales.nbytes // 4, scale, np.float32)
         self.scales.upload(ones)
@@ -99,3 +100,25 @@ def test_gated_block():
     for k, value in (("dgate_by_col", s * (2 - s)), ("dup_by_col", s), ("h_by_col", s)):
         last = grads[k].row(f - 1)
         assert last[t - 1] == 0x7E and not last[: t - 1].any() and abs(grads[k].scale(f - 1, t - 1) * 448 - value) < 1e-6
+
+
+def test_columns_in_the_longest_rows():
+    t, d, f = 40, 128, 200
+    print("backward pass, columns' forms in rows of 2^23 bytes", flush=True)
+    rng = np.random.default_rng(5)
+    dy, w, gate, up = Large(t, d), Large(f, d), Large(t, f), Large(t, f)
+    for m in (dy, w, gate, up):
+        for r in range(m.rows):
+            m.put(r, np.concatenate([fo.nearest_codes(rng.standard_normal(m.cols), fo.E4M3), np.zeros(-m.cols % 128)]))
+    given = dy.matrix, w.matrix, gate.matrix, up.matrix, B.CKPT_GATE_SILU, 0
+    forms = "dgate_by_col", "dup_by_col", "h_by_col"
+    plain = {k: Large(f, t, 0xEE) for k in forms}
+    B.gated_backward(*given, **{k: v.matrix for k, v in plain.items()})
+    for k in forms:
+        far = Large(f, t, 0xEE, pitch=1 << 23)
+        B.gated_backward(*given, **{k: far.matrix})
+        harness.synchronize()
+        for r in range(f):
+            assert np.array_equal(far.row(r, 0, 128), plain[k].row(r)) and np.all(far.row(r, 128, 128) == 0xEE), (k, r)
+            assert far.scale(r, 0) == plain[k].scale(r, 0)
+            assert plain[k].row(r)[:t].any()
