@@ -138,7 +138,7 @@ typedef enum { CKPT_GATE_SILU = 1, CKPT_GATE_GELU = 2 } ckpt_gate;
 
 /* Both projections, the activation, the product and the rounding to 8 bits in one pass. x is tokens x hidden, w_gate and w_up are ffn x hidden (CKPT_F8_E4M3,
  * blocks of one kind); gate, up and h are tokens x ffn, CKPT_F8_E4M3 with block_rows 1. gate and up are what the backward pass needs, rounded to 8
- * bits (h is made of the values before that rounding); both NULL: nothing is kept, as in serving. Workspace as in ckpt_f8_gemm, for few tokens. */
+ * bits (h is made of the values before that rounding); both NULL: nothing is kept, as in serving. Workspace as in ckpt_f8_gemm, for up to 64 tokens. */
 int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *bytes);
 int ckpt_gated_forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8_matrix *w_up, int32_t activation, const ckpt_f8_matrix *gate,
                        const ckpt_f8_matrix *up, const ckpt_f8_matrix *h, void *workspace, uint64_t workspace_bytes, void *stream);

@@ -67,6 +67,9 @@ inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool wide, bool ro
 // The gated block's forward pass: tiles of 256, 128 or 64 tokens by 128 columns of gate and of up, a block a unit, or (kGatedHalves) of 256 with the last round's in halves. By what a round of them costs, about microseconds: 4096 to 11008 columns
 // 64 tokens 38 us (60 by tiles of 128, 99 of 256), 256 tokens 65 (78 by 64, 98 by 256), 512 tokens 104 (122, 116), 1024 tokens 163 with halves (204 without, 185 by 128).
 constexpr int kGatedHalves = 3;
+// 17 to 64 tokens: tiles of 32 columns, whose values a second launch rounds, where they are at least half as many as the units and at most one round of two a unit. 4096 to 11008 columns 30 to 32 us (36 to 37 in one launch), 2048 to 8192 14 to 16 (21 to
+// 22), 8192 to 16384 72 to 77 (90), 768 to 4097, the fewest tiles, 12.4 to 13.5 (12.3 to 15); 8192 to 28672, 896 tiles, 127 (113).
+inline bool gated_values_first(uint64_t tokens, uint64_t ffn) { return tokens > kF8Few && tokens <= 64 && ffn > 32 * (kF8Units / 2 - 1) && ffn <= 32 * 2 * kF8Units; }
 inline int gated_form(uint64_t tokens, uint64_t across, uint32_t steps) {
     constexpr uint64_t rows[] = {256, 128, 64};
     constexpr double step[] = {2.75, 1.62, 0.97}, block[] = {10.6, 7.7, 6.9};

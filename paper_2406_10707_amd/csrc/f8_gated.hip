@@ -131,9 +131,9 @@ __global__ __launch_bounds__(512, 2) void gated_forward_halves_kernel(GatedForwa
     else if (int64_t(t.tm) * 256 + 128 * second < p.tokens) gated_forward_tile<Half, ACT, SQUARE, FA>(p, lds, int64_t(t.tm) * 256 + 128 * second, int64_t(t.tn) * 128);
 }
 
-// ------------------------------------------------------------------ up to sixteen tokens
+// ------------------------------------------------------------------ few tokens: values first
 
-// Rows of `pitch` floats, sixteen a matrix: h, then gate and up. No block has a whole block of 128 columns, so a second launch rounds them: 3 us of 22 for one token, 4096 to 11008 (90 MB; 18 us are this kernel's, 5.0 TB/s).
+// Up to sixteen tokens. Rows of `pitch` floats, one for each token: h, then gate and up. No block has a whole block of 128 columns, so a second launch rounds them: 3 us of 21 to 23 for one token, 4096 to 11008 (90 MB; 16.5 to 18 us are this kernel's, 5 TB/s and more).
 template <int WAVES, bool EIGHT, int ACT, int FA>
 __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(GatedForward p, float *values, uint64_t pitch) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[F8Few<WAVES, 2, EIGHT>::BYTES];
@@ -148,14 +148,41 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(GatedForward p, f
     float *at = values + (lane & 15) * pitch + n0 + 4 * (lane >> 4);
     *(f32x4 DSLLM_GLOBAL *)at = h;
     if (!p.gate.codes) return;
-    *(f32x4 DSLLM_GLOBAL *)(at + 16 * pitch) = sum[0];
-    *(f32x4 DSLLM_GLOBAL *)(at + 32 * pitch) = sum[1];
+    *(f32x4 DSLLM_GLOBAL *)(at + p.tokens * pitch) = sum[0];
+    *(f32x4 DSLLM_GLOBAL *)(at + 2 * p.tokens * pitch) = sum[1];
+}
+
+// Up to 64 tokens, values in the same rows: tiles of all tokens by 32 columns of gate and of up are four times as many as those with whole blocks of 128 (which of the two: gated_values_first).
+typedef F8Shape<2, 2, 2, 2, 1, 4, true> GatedValuesTile;
+template <int ACT, bool SQUARE, int FA>
+__global__ __launch_bounds__(256, 2) void gated_values_kernel(GatedForward p, float *values, uint64_t pitch) {
+    typedef GatedValuesTile S;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+    const int64_t col = int64_t(blockIdx.x) * (S::BN / 2);
+    const F8Loader<S> load(p.x, p.w_gate, p.w_up, p.steps, 0, col, lane, wave);
+    f32x4 acc[S::TM][S::TN];
+    f8_sums<S, SQUARE, true, FA, 0>(acc, lds, load, 0, p.steps, lane, wm, wn);
+    const int row = 16 * S::TM * wm + S::TM * (lane & 15);
+    float *at = values + row * pitch + col + 16 * wn + 4 * (lane >> 4);      // rows reach to a multiple of 128
+#pragma unroll
+    for (int i = 0; i < S::TM; i++, at += pitch) {
+        if (row + i >= p.tokens) return;
+        const f32x4 g = acc[i][0], u = acc[i][1];
+        f32x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; e++) h[e] = g[e] * sigmoid_of<ACT>(g[e]) * u[e];
+        *(f32x4 DSLLM_GLOBAL *)at = h;
+        if (!p.gate.codes) continue;
+        *(f32x4 DSLLM_GLOBAL *)(at + p.tokens * pitch) = g;
+        *(f32x4 DSLLM_GLOBAL *)(at + 2 * p.tokens * pitch) = u;
+    }
 }
 
 __global__ __launch_bounds__(256) void gated_round_kernel(GatedForward p, const float *values, uint64_t pitch) {
     const F8Held &to = blockIdx.y == 0 ? p.h : blockIdx.y == 1 ? p.gate : p.up;
-    const F8Source src{reinterpret_cast<const uint8_t *>(values + 16 * blockIdx.y * pitch), pitch, p.tokens, p.ffn, nullptr, 0, 0};
-    f8_round_rows<CKPT_F32>(src, to, 0, 512 * int64_t(blockIdx.x));
+    const F8Source src{reinterpret_cast<const uint8_t *>(values + p.tokens * blockIdx.y * pitch), pitch, p.tokens, p.ffn, nullptr, 0, 0};
+    f8_round_rows<CKPT_F32>(src, to, 16 * int64_t(blockIdx.z), 512 * int64_t(blockIdx.x));
 }
 
 // ------------------------------------------------------------------ backward
@@ -336,8 +363,9 @@ bool overlap(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b) {
     return uint64_t(a->codes) < codes_end(b) && uint64_t(b->codes) < codes_end(a);
 }
 
-uint64_t few_pitch(int64_t ffn) { return f8_padded(ffn); }
-uint64_t few_bytes(int64_t ffn) { return 3 * 16 * few_pitch(ffn) * sizeof(float); }
+// What the values of few tokens take, 0 where they are rounded in one launch.
+uint64_t values_pitch(int64_t ffn) { return f8_padded(ffn); }
+uint64_t values_bytes(int64_t tokens, int64_t ffn) { return uint64_t(tokens) <= kF8Few || gated_values_first(uint64_t(tokens), uint64_t(ffn)) ? 3 * tokens * values_pitch(ffn) * sizeof(float) : 0; }
 
 int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8_matrix *w_up, int32_t activation, const ckpt_f8_matrix *gate, const ckpt_f8_matrix *up, const ckpt_f8_matrix *h,
             void *workspace, uint64_t workspace_bytes, hipStream_t stream) {
@@ -368,17 +396,21 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
     const GatedForward p{f8_side(x), f8_side(w_gate), f8_side(w_up), F8Held(gate), F8Held(up), F8Held(h), tokens, ffn, steps};
     const bool x_e5m2 = x->format == CKPT_F8_E5M2;
     const int64_t across = (ffn + 127) / 128;
-    if (uint64_t(tokens) <= kF8Few && steps && workspace && workspace_bytes >= few_bytes(ffn) && across < 1 << 20) {
+    const uint64_t bytes = values_bytes(tokens, ffn);
+    if (bytes && steps && workspace && workspace_bytes >= bytes && across < 1 << 20) {
         if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
-        if (const char *why = ranges.wrong(workspace, few_bytes(ffn))) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
+        if (const char *why = ranges.wrong(workspace, bytes)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
         float *values = static_cast<float *>(workspace);
-        const uint64_t pitch = few_pitch(ffn);
-        with_kinds(activation, x_e5m2, true, [&](auto act, auto fa, auto) {
-            auto launch = [&](auto waves, auto eight) { hipLaunchKernelGGL((gated_few_kernel<waves, eight, act, fa>), dim3(unsigned((ffn + 15) / 16)), dim3(64 * waves), 0, stream, p, values, pitch); };
-            if (f8_few_waves(uint64_t(ffn), steps) == 2) tokens <= 8 ? launch(std::integral_constant<int, 2>(), std::true_type()) : launch(std::integral_constant<int, 2>(), std::false_type());
-            else tokens <= 8 ? launch(std::integral_constant<int, 4>(), std::true_type()) : launch(std::integral_constant<int, 4>(), std::false_type());
-        });
-        hipLaunchKernelGGL(gated_round_kernel, dim3(unsigned((ffn + 511) / 512), gate ? 3 : 1), dim3(256), 0, stream, p, values, pitch);
+        const uint64_t pitch = values_pitch(ffn);
+        if (uint64_t(tokens) > kF8Few)
+            with_kinds(activation, x_e5m2, p.w_gate.shift, [&](auto act, auto fa, auto square) { hipLaunchKernelGGL((gated_values_kernel<act, square, fa>), dim3(unsigned((ffn + 31) / 32)), dim3(256), 0, stream, p, values, pitch); });
+        else
+            with_kinds(activation, x_e5m2, true, [&](auto act, auto fa, auto) {
+                auto launch = [&](auto waves, auto eight) { hipLaunchKernelGGL((gated_few_kernel<waves, eight, act, fa>), dim3(unsigned((ffn + 15) / 16)), dim3(64 * waves), 0, stream, p, values, pitch); };
+                if (f8_few_waves(uint64_t(ffn), steps) == 2) tokens <= 8 ? launch(std::integral_constant<int, 2>(), std::true_type()) : launch(std::integral_constant<int, 2>(), std::false_type());
+                else tokens <= 8 ? launch(std::integral_constant<int, 4>(), std::true_type()) : launch(std::integral_constant<int, 4>(), std::false_type());
+            });
+        hipLaunchKernelGGL(gated_round_kernel, dim3(unsigned((ffn + 511) / 512), gate ? 3 : 1, unsigned((tokens + 15) / 16)), dim3(256), 0, stream, p, values, pitch);
         return launched();
     }
     auto tiles = [&](auto shape) {
@@ -464,7 +496,7 @@ int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *
         if (!bytes || tokens < 0 || ffn < 0 || hidden < 0) return refuse(CKPT_EINVAL, "null argument or negative size");
         *bytes = 0;
         if (tokens > 0x7FFFFFFF || ffn > 0x7FFFFFFF || hidden > kF8LongestRow) return refuse(CKPT_EINVAL, "a side is over 2^31 - 1, or what is contracted over 2^23");
-        if (tokens && ffn && hidden && uint64_t(tokens) <= kF8Few) *bytes = few_bytes(ffn);
+        if (tokens && ffn && hidden) *bytes = values_bytes(tokens, ffn);
         return int(CKPT_OK);
     });
 }

@@ -183,6 +183,7 @@ int main() {
     tiles<F8Shape<4, 2, 4, 8, 4, 2, true>>("pair 256x256");
     tiles<F8Shape<4, 2, 2, 8, 4, 2, true>>("pair 128x256");
     tiles<F8Shape<2, 4, 2, 4, 2, 2, true>>("pair 64x256");
+    tiles<F8Shape<2, 2, 2, 2, 1, 4, true>>("pair 64x64");
     few<1, false>();
     few<1, true>();
     few<2, false>();

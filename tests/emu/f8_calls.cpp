@@ -176,6 +176,19 @@ void refusals() {
     REQUIRE(launches.size() == 2);
     TAKEN(ckpt_gated_forward(&x1, &wg, &wu, CKPT_GATE_SILU, nullptr, nullptr, &h1, fws, bytes - 1, nullptr));
     REQUIRE(launches.size() == 1);
+    const auto x64 = matrix(CKPT_F8_E4M3, 64, 200), w4096 = matrix(CKPT_F8_E4M3, 4096, 200, 128), u4096 = matrix(CKPT_F8_E4M3, 4096, 200, 128), h64 = matrix(CKPT_F8_E4M3, 64, 4096), g64 = matrix(CKPT_F8_E4M3, 64, 4096),
+               p64 = matrix(CKPT_F8_E4M3, 64, 4096);
+    uint64_t values;
+    REQUIRE(ckpt_gated_workspace(64, 4096, 200, &values) == CKPT_OK && values == 3ull * 64 * 4096 * 4);
+    char *vws = static_cast<char *>(allocate(values));
+    for (const ckpt_f8_matrix *gate64 : {static_cast<const ckpt_f8_matrix *>(nullptr), &g64}) {
+        TAKEN(ckpt_gated_forward(&x64, &w4096, &u4096, CKPT_GATE_SILU, gate64, gate64 ? &p64 : nullptr, &h64, vws, values, nullptr));
+        REQUIRE(launches.size() == 2);
+        TAKEN(ckpt_gated_forward(&x64, &w4096, &u4096, CKPT_GATE_SILU, gate64, gate64 ? &p64 : nullptr, &h64, vws, values - 1, nullptr));
+        REQUIRE(launches.size() == 1);
+    }
+    REFUSED(ckpt_gated_forward(&x64, &w4096, &u4096, CKPT_GATE_SILU, nullptr, nullptr, &h64, vws + 8, values, nullptr));
+    REFUSED(ckpt_gated_forward(&x64, &w4096, &u4096, CKPT_GATE_SILU, nullptr, nullptr, &h64, vws + 16, values, nullptr));
     REFUSED(ckpt_gated_forward(&x1, &wg, &wu, CKPT_GATE_SILU, nullptr, nullptr, &h1, fws + 4, bytes, nullptr));
     REFUSED(ckpt_gated_forward(&x1, &wg, &wu, CKPT_GATE_SILU, nullptr, nullptr, &h1, fws + (1 << 21), bytes, nullptr));
     // backward

@@ -80,6 +80,20 @@ def test_forward_tiles(t, d, f, block_rows):
     check_forward(t, d, f, "silu", True, fo.E4M3, fo.E4M3, block_rows, t)
 
 
+# 17 to 64 tokens by tiles of 32 columns, rounded by a second launch: the fewest and the most tiles, whole and ragged
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_forward_values_first(block_rows, name):
+    for case, (t, d, f) in enumerate([(17, 300, 4090), (64, 129, 4224), (33, 640, 5003), (48, 1, 4097), (40, 256, 16384)]):
+        need = B.gated_workspace(t, f, d)
+        assert need
+        for keep in (False, True):
+            check_forward(t, d, f, name, keep, (fo.E4M3, fo.E5M2)[case % 2], fo.E4M3, block_rows, case)
+    check_forward(33, 640, 5003, name, True, fo.E4M3, fo.E4M3, block_rows, 2, use_workspace=False)
+    for t, f in ((17, 4064), (64, 16385), (65, 8192)):
+        assert B.gated_workspace(t, f, 256) == 0
+
+
 BACKWARD = [(1, 1, 1), (1, 64, 128), (3, 100, 300), (16, 128, 64), (63, 129, 127), (127, 300, 129), (128, 128, 128), (129, 256, 257), (200, 1000, 130), (256, 384, 512), (300, 768, 2050), (1000, 200, 300)]
 GRADS = ("dgate", "dup", "dgate_by_col", "dup_by_col", "h_by_col")
 
