@@ -294,7 +294,7 @@ __device__ __forceinline__ void f8_sums(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds
 
 // As single tokens give them: B is what has to be read, once, at the rate of memory. A block takes 16 rows of B (of each of MATRICES); its waves take the windows of four steps in turn, each with LDS of its own, so that none waits
 // for another before the sums are added, in wave order. Four steps of B and A are under way a wave; a step's place is filled again as soon as it has been read. One row through 4096 x 11008 10 us from memory that the last level of cache
-// holds in part, 12.8 from HBM (3.5 TB/s: a launch and eleven windows of a wave in a row), through 28672 x 8192 42 (5.6 TB/s).
+// holds in part, 12.8 from HBM (3.5 TB/s: a launch, then five or six windows of a wave in a row), through 28672 x 8192 42 (5.6 TB/s).
 template <int WAVES, int MATRICES, bool EIGHT>
 struct F8Few {
     typedef F8FewLoader<MATRICES, EIGHT> Loader;
