@@ -120,8 +120,8 @@ int ckpt_f8_dequantize(const ckpt_f8_matrix *src, void *dst, int32_t dst_dtype, 
 
 /* C = A * B^T, or C += A * B^T with accumulate != 0. A is M x K, B is N x K, in either format and blocks of either kind; C is row-major, CKPT_BF16, CKPT_F16 or
  * CKPT_F32, aligned to its element, `ldc` elements from row to row. The products of a block are summed on the matrix cores and,
- * times both scales (whose product f32 has to hold), added in f32; one rounding at the end. For C in 16 bits and more than sixteen rows of A these sums are those of the 8-bit matrix instructions, which cut products
- * more than 13 bits below the largest of eight; for C in f32, and for up to sixteen rows, they are sums in f32. A linear layer y = x W^T takes (x, W) forward, (dy, W by
+ * times both scales (whose product f32 has to hold), added in f32; one rounding at the end. For C in bf16 and more than sixteen rows of A these sums are those of the 8-bit matrix instructions, which cut products
+ * more than 13 bits below the largest of eight; for C in f32 and f16, and for up to sixteen rows, they are sums in f32. A linear layer y = x W^T takes (x, W) forward, (dy, W by
  * columns) for dx and (dy by columns, x by columns) for dW. Some sizes split K among blocks and need workspace: ckpt_f8_gemm_workspace bytes (16-byte
  * aligned, contents do not matter, not shared by calls that may overlap); with less (or NULL) the call runs with fewer parts or unsplit.
  * C must not overlap A, B or the workspace. */

@@ -5,7 +5,7 @@
 namespace dsllm {
 
 // A form's tile, how many of its blocks share a compute unit, and what it costs, about microseconds, fitted to 1500 times of 32 products from 300 x 2050 x 768 to 8192^3: a step of 128 values of K with blocks on every unit (and in
-// every round but the last) or, of forms whose blocks share a unit, with one on it; what a block takes besides, with C in 16 bits or in f32. Steps for the two kinds of sums (8-bit instructions, bf16) and of B's scales (of 128 x 128,
+// every round but the last) or, of forms whose blocks share a unit, with one on it; what a block takes besides, with C in bf16 or in f32 (as which f16 counts). Steps for the two kinds of sums (8-bit instructions, bf16) and of B's scales (of 128 x 128,
 // of single rows). The choice is in the mean 1 % over the best
 // form, at most 8 %.
 struct F8Form {

@@ -111,10 +111,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void f8_gemm_kernel(F8Gemm p, TileOr
         else store_sums<S, dtype, false>(p, acc, lds, row, col, lane, wave, wm, wn);
     };
     if (p.dtype == CKPT_F32) out(std::integral_constant<int, CKPT_F32>());
-    else if constexpr (!WIDE) {
-        if (p.dtype == CKPT_BF16) out(std::integral_constant<int, CKPT_BF16>());
-        else out(std::integral_constant<int, CKPT_F16>());
-    }
+    else out(std::integral_constant<int, WIDE ? CKPT_F16 : CKPT_BF16>());
 }
 
 // ------------------------------------------------------------------ up to sixteen rows of A
@@ -232,7 +229,7 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
     if (k == 0 && accumulate) return CKPT_OK;
     const uint32_t steps = f8_steps(uint64_t(k));
     F8Gemm p{f8_side(a), f8_side(b), c, ldc, m, n, steps, steps, 0, accumulate, dtype};
-    const bool a_e5m2 = a->format == CKPT_F8_E5M2, b_e5m2 = b->format == CKPT_F8_E5M2, wide = dtype == CKPT_F32;
+    const bool a_e5m2 = a->format == CKPT_F8_E5M2, b_e5m2 = b->format == CKPT_F8_E5M2, wide = dtype != CKPT_BF16;
     if (uint64_t(m) <= kF8Few) {
         const uint32_t waves = f8_few_waves(uint64_t(n), steps);
         launch_in_parts(p, 128, 16ll << 22, [&](const F8Gemm &part) {
