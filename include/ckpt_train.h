@@ -90,8 +90,8 @@ typedef enum { CKPT_F8_E4M3 = 3, CKPT_F8_E5M2 = 4 } ckpt_f8_format;
  * 128, codes 16-byte aligned; between cols and that multiple a row's codes are zero (every call here writes them so and relies on it), what
  * the pitch has beyond is not touched. Half the columns of a wider matrix are such a matrix where they begin at a multiple of 128. Scales
  * lie by blocks of columns, so that a product reads those of neighbouring rows at once: that of element (r, c) is
- * scales[(c / 128) * scale_pitch + r / block_rows], scale_pitch at least ceil(rows / block_rows). Matrices that a call writes may not
- * overlap what it reads. cols is at most 2^23 where a product contracts over them. */
+ * scales[(c / 128) * scale_pitch + r / block_rows], scale_pitch at least ceil(rows / block_rows). What a call writes (codes,
+ * scales, plain matrices, workspace) may share no byte with anything else that it reads or writes, and is refused if it does; rows may lie between another's rows. cols is at most 2^23 where a product contracts over them. */
 typedef struct {
     int32_t format;        /* ckpt_f8_format */
     int32_t block_rows;    /* 1 or 128 */

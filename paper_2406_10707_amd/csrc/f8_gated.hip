@@ -352,17 +352,6 @@ void with_kinds(int32_t activation, bool e5m2, bool square, F f) {
 bool fits_grid(int64_t down, int64_t across) { return down * across < 1 << 22; }
 constexpr const char *kTooManyTiles = "more than 2^22 tiles of tokens and columns";
 
-bool overlap(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b) {
-    if (!a || !b || !a->rows || !a->cols || !b->rows || !b->cols) return false;
-    auto codes_end = [](const ckpt_f8_matrix *m) { return uint64_t(m->codes) + (uint64_t(m->rows) - 1) * m->code_pitch + f8_padded(m->cols); };
-    if (a->code_pitch == b->code_pitch && uint64_t(a->codes) < codes_end(b) && uint64_t(b->codes) < codes_end(a)) {      // halves of a wider matrix lie between one another's rows
-        const uint64_t pitch = a->code_pitch, apart = (uint64_t(a->codes) > uint64_t(b->codes) ? uint64_t(a->codes) - uint64_t(b->codes) : uint64_t(b->codes) - uint64_t(a->codes)) % pitch;
-        const bool a_first = uint64_t(a->codes) <= uint64_t(b->codes);
-        return apart < f8_padded(a_first ? a->cols : b->cols) || apart + f8_padded(a_first ? b->cols : a->cols) > pitch;
-    }
-    return uint64_t(a->codes) < codes_end(b) && uint64_t(b->codes) < codes_end(a);
-}
-
 // What the values of few tokens take, 0 where they are rounded in one launch.
 uint64_t values_pitch(int64_t ffn) { return f8_padded(ffn); }
 uint64_t values_bytes(int64_t tokens, int64_t ffn) { return uint64_t(tokens) <= kF8Few || gated_values_first(uint64_t(tokens), uint64_t(ffn)) ? 3 * tokens * values_pitch(ffn) * sizeof(float) : 0; }
@@ -388,8 +377,9 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
         if (every[i].m) {
             if (every[i].m->rows != tokens || every[i].m->cols != ffn) return refuse(CKPT_EINVAL, std::string(every[i].name) + "not tokens x ffn");
             if (every[i].m->block_rows != 1 || every[i].m->format != CKPT_F8_E4M3) return refuse(CKPT_EINVAL, std::string(every[i].name) + "must be CKPT_F8_E4M3 with block_rows 1");
+            if (overlaps_itself(*every[i].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "codes and scales overlap");
             for (int k = 0; k < i; k++)
-                if (overlap(every[i].m, every[k].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "overlaps another matrix");
+                if (every[k].m && overlap(*every[i].m, *every[k].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "overlaps another matrix");
         }
     if (tokens == 0 || ffn == 0) return CKPT_OK;
     const uint32_t steps = f8_steps(uint64_t(x->cols));
@@ -400,6 +390,8 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
     if (bytes && steps && workspace && workspace_bytes >= bytes && across < 1 << 20) {
         if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
         if (const char *why = ranges.wrong(workspace, bytes)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
+        for (const auto &e : every)
+            if (e.m && overlap(*e.m, Rows{uint64_t(workspace), bytes, bytes, 1})) return refuse(CKPT_EINVAL, std::string("workspace: overlaps ") + e.name);
         float *values = static_cast<float *>(workspace);
         const uint64_t pitch = values_pitch(ffn);
         if (uint64_t(tokens) > kF8Few)
@@ -470,8 +462,9 @@ int backward(const ckpt_f8_matrix *dy, const ckpt_f8_matrix *w_down, const ckpt_
             if (every[i].m->rows != (i < 6 ? tokens : ffn) || every[i].m->cols != (i < 6 ? ffn : tokens)) return refuse(CKPT_EINVAL, std::string(every[i].name) + (i < 6 ? "not tokens x ffn" : "not ffn x tokens"));
             if (every[i].m->block_rows != 1) return refuse(CKPT_EINVAL, std::string(every[i].name) + "block_rows must be 1");
             if ((i < 4 || i == 8) && every[i].m->format != CKPT_F8_E4M3) return refuse(CKPT_EINVAL, std::string(every[i].name) + "must be CKPT_F8_E4M3");
+            if (i >= 4 && overlaps_itself(*every[i].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "codes and scales overlap");
             for (int k = 0; i >= 4 && k < i; k++)
-                if (overlap(every[i].m, every[k].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "overlaps another matrix");
+                if (every[k].m && overlap(*every[i].m, *every[k].m)) return refuse(CKPT_EINVAL, std::string(every[i].name) + "overlaps another matrix");
         }
     if (tokens == 0 || ffn == 0) return CKPT_OK;
     const GatedBackward p{f8_side(dy), f8_side(w_down), F8Held(gate), F8Held(up), F8Held(grads->dgate), F8Held(grads->dup), F8Held(grads->dgate_by_col), F8Held(grads->dup_by_col), F8Held(grads->h_by_col),

@@ -226,6 +226,8 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
     if (ldc < n || ldc > (1ll << 48) / m) return refuse(CKPT_EINVAL, "ldc is smaller than a row, or C too large");
     if (uint64_t(c) % bytes) return refuse(CKPT_EINVAL, "C is not aligned to its element");
     if (const char *why = ranges.wrong(c, (uint64_t(m - 1) * ldc + n) * bytes)) return refuse(CKPT_EINVAL, std::string("C: ") + why);
+    const Rows c_rows = plain_rows(c, m, n, ldc, bytes);
+    if (overlap(*a, c_rows) || overlap(*b, c_rows)) return refuse(CKPT_EINVAL, "C: overlaps A or B");
     if (k == 0 && accumulate) return CKPT_OK;
     const uint32_t steps = f8_steps(uint64_t(k));
     F8Gemm p{f8_side(a), f8_side(b), c, ldc, m, n, steps, steps, 0, accumulate, dtype};
@@ -248,7 +250,10 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
         return launched();
     }
     if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
-    if (const char *why = ranges.wrong(workspace, f8_part_bytes(uint64_t(m), uint64_t(n)) * choice.splits)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
+    const uint64_t part_bytes = f8_part_bytes(uint64_t(m), uint64_t(n)) * choice.splits;
+    if (const char *why = ranges.wrong(workspace, part_bytes)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
+    const Rows part_rows{uint64_t(workspace), part_bytes, part_bytes, 1};
+    if (overlap(*a, part_rows) || overlap(*b, part_rows) || share_bytes(c_rows, part_rows)) return refuse(CKPT_EINVAL, "workspace: overlaps A, B or C");
     const uint32_t pitch = uint32_t(f8_part_pitch(uint64_t(n)));
     F8Gemm parts = p;
     parts.c = workspace;

@@ -289,6 +289,9 @@ int quantize(const void *src, int32_t dtype, int64_t ld, const ckpt_f8_matrix *b
     if (ld < cols || ld > (1ll << 48) / rows) return refuse(CKPT_EINVAL, "ld is smaller than a row, or the matrix too large");
     if (uint64_t(src) % bytes) return refuse(CKPT_EINVAL, "src is not aligned to its element");
     if (const char *why = ranges.wrong(src, (uint64_t(rows - 1) * ld + cols) * bytes)) return refuse(CKPT_EINVAL, std::string("src: ") + why);
+    for (const ckpt_f8_matrix *m : {by_row, by_col})
+        if (m && (overlaps_itself(*m) || overlap(*m, plain_rows(src, rows, cols, ld, bytes)))) return refuse(CKPT_EINVAL, std::string(m == by_row ? "by_row: " : "by_col: ") + "overlaps src or itself");
+    if (by_row && by_col && overlap(*by_row, *by_col)) return refuse(CKPT_EINVAL, "by_row and by_col overlap");
     const F8Source from{static_cast<const uint8_t *>(src), uint64_t(ld), rows, cols, nullptr, 0, 0};
     const bool square = (by_row ? by_row : by_col)->block_rows == 128;
     switch (dtype) {
@@ -307,6 +310,7 @@ int columns(const ckpt_f8_matrix *src, const ckpt_f8_matrix *by_col, hipStream_t
     if (src->block_rows != by_col->block_rows) return refuse(CKPT_EINVAL, "src and by_col differ in block_rows");
     if (src->block_rows == 128 && src->format != by_col->format) return refuse(CKPT_EINVAL, "src and by_col differ in their format: with block_rows 128 the values stay as they are");
     if (src->rows == 0 || src->cols == 0) return CKPT_OK;
+    if (overlaps_itself(*by_col) || overlap(*by_col, *src)) return refuse(CKPT_EINVAL, "by_col: overlaps src or itself");
     const F8Source from{static_cast<const uint8_t *>(src->codes), src->code_pitch, src->rows, src->cols, src->scales, src->scale_pitch, src->format == CKPT_F8_E5M2};
     const uint64_t down = (uint64_t(src->rows) + 127) / 128, across = (uint64_t(src->cols) + 127) / 128;
     if (!fits_grid(down, across)) return refuse(CKPT_EINVAL, kTooLarge);
@@ -325,6 +329,7 @@ int dequantize(const ckpt_f8_matrix *m, void *dst, int32_t dtype, int64_t ld, hi
     if (ld < m->cols || ld > (1ll << 48) / m->rows) return refuse(CKPT_EINVAL, "ld is smaller than a row, or the matrix too large");
     if (uint64_t(dst) % bytes) return refuse(CKPT_EINVAL, "dst is not aligned to its element");
     if (const char *why = ranges.wrong(dst, (uint64_t(m->rows - 1) * ld + m->cols) * bytes)) return refuse(CKPT_EINVAL, std::string("dst: ") + why);
+    if (overlap(*m, plain_rows(dst, m->rows, m->cols, ld, bytes))) return refuse(CKPT_EINVAL, "dst: overlaps src");
     const uint64_t pieces = (uint64_t(m->cols) + 511) / 512;
     if (uint64_t(m->rows) > 1ull << 26 || !fits_grid((m->rows + 3) / 4, pieces)) return refuse(CKPT_EINVAL, kTooLarge);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned((m->rows * pieces + 3) / 4)), dim3(256), 0, stream, F8Held(m), static_cast<uint8_t *>(dst), uint64_t(ld), uint32_t(pieces)); };
@@ -350,6 +355,27 @@ const char *dsllm::wrong_f8_matrix(const ckpt_f8_matrix *m, DeviceRanges &ranges
     if (const char *why = ranges.wrong(m->codes, (rows - 1) * m->code_pitch + padded)) return why;
     return ranges.wrong(m->scales, 4 * ((padded / 128 - 1) * m->scale_pitch + scale_rows));
 }
+
+bool dsllm::share_bytes(const Rows &a, const Rows &b) {
+    if (a.at >= b.end() || b.at >= a.end()) return false;
+    if (a.pitch == b.pitch) {
+        const Rows &first = a.at <= b.at ? a : b, &second = a.at <= b.at ? b : a;
+        const uint64_t apart = (second.at - first.at) % a.pitch;
+        return apart < first.width || apart + second.width > a.pitch;
+    }
+    const Rows &few = a.rows <= b.rows ? a : b, &many = a.rows <= b.rows ? b : a;
+    if (few.rows > 1 << 16) return true;
+    for (uint64_t r = 0; r < few.rows; r++) {
+        const uint64_t lo = few.at + r * few.pitch, hi = lo + few.width, k = lo < many.at + many.width ? 0 : (lo - many.at - many.width) / many.pitch + 1;      // the first row of the other that ends behind lo
+        if (k < many.rows && many.at + k * many.pitch < hi) return true;
+    }
+    return false;
+}
+static Rows codes_of(const ckpt_f8_matrix &m) { return Rows{uint64_t(m.codes), f8_padded(m.cols), m.code_pitch, uint64_t(m.rows)}; }
+static Rows scales_of(const ckpt_f8_matrix &m) { return Rows{uint64_t(m.scales), 4 * ((uint64_t(m.rows) + m.block_rows - 1) / m.block_rows), 4 * m.scale_pitch, f8_padded(m.cols) / 128}; }
+bool dsllm::overlap(const ckpt_f8_matrix &m, const Rows &rows) { return m.rows && m.cols && (share_bytes(codes_of(m), rows) || share_bytes(scales_of(m), rows)); }
+bool dsllm::overlap(const ckpt_f8_matrix &a, const ckpt_f8_matrix &b) { return a.rows && a.cols && (overlap(b, codes_of(a)) || overlap(b, scales_of(a))); }
+bool dsllm::overlaps_itself(const ckpt_f8_matrix &m) { return m.rows && m.cols && share_bytes(codes_of(m), scales_of(m)); }
 
 extern "C" {
 

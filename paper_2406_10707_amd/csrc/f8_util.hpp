@@ -8,6 +8,20 @@ namespace dsllm {
 const char *wrong_f8_matrix(const ckpt_f8_matrix *m, DeviceRanges &ranges);
 
 inline uint64_t f8_padded(int64_t cols) { return (uint64_t(cols) + 127) / 128 * 128; }
+
+// `rows` of `width` bytes, `pitch` apart, from address `at` on
+struct Rows {
+    uint64_t at, width, pitch, rows;
+    uint64_t end() const { return at + (rows - 1) * pitch + width; }
+};
+inline Rows plain_rows(const void *p, int64_t rows, int64_t cols, int64_t ld, uint32_t bytes) { return Rows{uint64_t(p), uint64_t(cols) * bytes, uint64_t(ld) * bytes, uint64_t(rows)}; }
+// Whether they have a byte in common. Rows may lie between one another's; of different pitches, and more than 2^16 rows on both sides that lie in one range, they are taken to have.
+bool share_bytes(const Rows &a, const Rows &b);
+// Whether codes or scales do. An empty matrix shares nothing.
+bool overlap(const ckpt_f8_matrix &a, const ckpt_f8_matrix &b);
+bool overlap(const ckpt_f8_matrix &m, const Rows &rows);
+bool overlaps_itself(const ckpt_f8_matrix &m);      // its codes with its scales
+
 inline uint32_t f8_row_shift(const ckpt_f8_matrix &m) { return m.block_rows == 128 ? 7 : 0; }
 
 // A matrix as kernels read or write it; codes nullptr: not wanted
