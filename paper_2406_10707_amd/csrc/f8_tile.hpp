@@ -3,8 +3,10 @@
 //
 // A block's products are summed by the matrix instructions, from zero; the vector units add the sum, times the two scales, to the f32 sums: four multiply-adds for 16 x 16 elements of C a lane. Sums therefore lie in ordinary
 // registers, not in accumulation registers, which the vector units cannot read. There are two ways to a block's sum:
-//   * v_mfma_f32_16x16x128_f8f6f4 takes the codes: 128 is a block. It adds eight products at a time in a window of 14 bits below the largest of them (measured: 2^16 + 2^2 loses the 2^2, 2^16 + 2^3 does not; between eights nothing
-//     is lost), so that a sum is off by 1.5e-5 of its size in the mean over normally distributed data, at most some 2^-16 of the sum of magnitudes. For results in bf16, whose rounding is 2^-8; half a step of f16, 2^-11, is no more than what is cut.
+//   * v_mfma_f32_16x16x128_f8f6f4 takes the codes: 128 is a block. It adds eight products, of consecutive elements, at a time, each cut to a multiple of 2^-13 of 2^e, e the largest sum of two exponents among the eight
+//     (a subnormal code has the smallest normal one's). Measured: beside 2^16, 2^3 stays, 15 becomes 8 and 7 becomes 0; between eights nothing is lost. So an eight is off by less than 7 * 2^-13 of its largest product, a sum by less than
+//     2^-10 of the sum of magnitudes (of normal codes; an eight of subnormal ones by up to 2^3 more of its own products). In the mean over normally distributed data it is 1.5e-5 of the sum's size. The worst is a quarter of what the
+//     rounding of a result to bf16 may be off by, 2^-8 of it, unless large products cancel: what stood beside them is lost then. Only for C in bf16: half a step of f16 is 2^-11.
 //   * WIDE: v_mfma_f32_16x16x32_bf16, four times, of the codes as bf16, which holds them: half the rate, and sums as f32 gives them (1e-8). For results in f32 and f16, and for those that are rounded to 8 bits, whose scales are f32.
 //
 // B goes first: a lane then holds four consecutive columns of one row of C. Fragments of rows of A and B hold rows in an order of their own (below), so that a lane ends up with 4 TNG consecutive columns of TM consecutive rows.
