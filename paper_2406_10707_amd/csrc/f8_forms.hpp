@@ -23,6 +23,7 @@ constexpr F8Form kF8Forms[] = {
     {"64x64", 64, 64, 2, {{0.22, 0.38}, {0.27, 0.41}, {0.47, 0.65}, {0.52, 0.73}}, {2.8, 2.5}},
 };
 constexpr int kF8FormCount = sizeof(kF8Forms) / sizeof(kF8Forms[0]);
+constexpr bool f8_form_has(int form, bool wide, bool rows) { return kF8Forms[form].step[2 * wide + rows][1] < kF8Never; }
 constexpr uint32_t kF8Units = 256;
 constexpr double kF8Join = 3.0, kF8JoinSplit = 0.45, kF8JoinBytes = 11.9e6;      // what joining parts of K costs besides, for each part, bytes a unit of cost
 constexpr uint64_t kF8MostTiles = 1u << 22;              // of a launch
@@ -51,15 +52,15 @@ struct F8Choice { int form; uint32_t splits; };
 // The cheapest form and number of parts whose parts fit the workspace. Joining the parts costs another launch and the way of the parts to memory and back.
 inline F8Choice f8_choice(uint64_t m, uint64_t n, uint64_t k, bool wide, bool rows, uint64_t workspace) {
     const uint32_t steps = f8_steps(k);
-    F8Choice best{0, 1};
+    F8Choice best{-1, 1};
     double least = 0;
     for (int f = 0; f < kF8FormCount; f++)
-        for (uint32_t splits = 1; splits <= 16; splits *= 2) {
+        for (uint32_t splits = 1; splits <= 16 && f8_form_has(f, wide, rows); splits *= 2) {
             const uint32_t each = (steps + splits - 1) / splits;
             if (splits > 1 && (uint64_t(each) * (splits - 1) >= steps || f8_part_bytes(m, n) > workspace / splits || kF8Forms[f].tiles(m, n) > kF8MostTiles || m * f8_part_pitch(n) >> 33)) break;      // one launch for the tiles, one of 2^31 threads at most that joins them
             double t = f8_cost(kF8Forms[f], m, n, each, splits, wide, rows);
             if (splits > 1) t += kF8Join + kF8JoinSplit * splits + double(f8_part_bytes(m, n)) * (2 * splits + 1) / kF8JoinBytes;
-            if ((f == 0 && splits == 1) || t < least) { best = F8Choice{f, splits}; least = t; }
+            if (best.form < 0 || t < least) { best = F8Choice{f, splits}; least = t; }
         }
     return best;
 }

@@ -182,33 +182,38 @@ void launch_in_parts(const F8Gemm &p, int64_t rows, int64_t columns, F launch) {
         }
 }
 
-// In the order of kF8Forms
-void launch_form(const F8Choice &choice, const F8Gemm &p, bool wide, bool a_e5m2, bool b_e5m2, hipStream_t stream) {
+// False: the form has no kernel for these sums and scales, and nothing was launched.
+bool launch_form(const F8Choice &choice, const F8Gemm &p, bool wide, bool a_e5m2, bool b_e5m2, hipStream_t stream) {
+    if (choice.form < 0 || !f8_form_has(choice.form, wide, !p.b.shift)) return false;
     const F8Form &f = kF8Forms[choice.form];
     const int64_t tiles_each = std::max<int64_t>(1, std::min<int64_t>((p.n + f.bn - 1) / f.bn, int64_t(kF8MostTiles)));
     const int64_t columns = tiles_each * f.bn, rows = std::max<int64_t>(1, int64_t(kF8MostTiles) / tiles_each) * f.bm;
     launch_in_parts(p, (rows + 127) / 128 * 128, (columns + 127) / 128 * 128, [&](const F8Gemm &part) {
         const uint32_t tiles_m = uint32_t((part.m + f.bm - 1) / f.bm), tiles_n = uint32_t((part.n + f.bn - 1) / f.bn);
         with_formats(a_e5m2, b_e5m2, [&](auto fa, auto fb) {
-            auto go = [&](auto shape) {
-                typedef decltype(shape) S;
+            auto go = [&](auto form) {
+                typedef typename F8GemmShape<form>::type S;
+                static_assert(S::BM == kF8Forms[form].bm && S::BN == kF8Forms[form].bn, "the table's tile");
                 const dim3 grid(tiles_m * tiles_n, choice.splits), block(S::THREADS);
                 const TileOrder order(tiles_m, tiles_n, true);
                 auto launch = [&](auto square, auto wide_) {
-                    if constexpr (square || wide_ || S::BN < 256) hipLaunchKernelGGL((f8_gemm_kernel<S, square, wide_, fa, fb>), grid, block, 0, stream, part, order);      // kF8Never
+                    if constexpr (f8_form_has(form, wide_, !square)) hipLaunchKernelGGL((f8_gemm_kernel<S, square, wide_, fa, fb>), grid, block, 0, stream, part, order);
                 };
                 if (part.b.shift) wide ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
                 else wide ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
             };
             switch (choice.form) {
-                case 0: go(F8Shape<4, 2, 4, 8, 4, 2, false>()); break;
-                case 1: go(F8Shape<4, 2, 4, 4, 4, 3, false>()); break;
-                case 2: go(F8Shape<2, 2, 4, 4, 4, 2, false>()); break;
-                default: go(F8Shape<2, 2, 2, 2, 2, 4, false>()); break;
+                case 0: go(std::integral_constant<int, 0>()); break;
+                case 1: go(std::integral_constant<int, 1>()); break;
+                case 2: go(std::integral_constant<int, 2>()); break;
+                default: go(std::integral_constant<int, 3>()); break;
             }
+            static_assert(kF8FormCount == 4, "every form is launched");
         });
     });
+    return true;
 }
+constexpr const char *kNoForm = "no kernel for a product of this size";
 
 int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtype, int64_t ldc, int32_t accumulate, void *workspace, uint64_t workspace_bytes, hipStream_t stream) {
     if (!a || !b) return refuse(CKPT_EINVAL, "null argument");
@@ -245,10 +250,7 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
         return launched();
     }
     const F8Choice choice = f8_choice(uint64_t(m), uint64_t(n), uint64_t(k), wide, !p.b.shift, workspace ? workspace_bytes : 0);
-    if (choice.splits == 1) {
-        launch_form(choice, p, wide, a_e5m2, b_e5m2, stream);
-        return launched();
-    }
+    if (choice.splits == 1) return launch_form(choice, p, wide, a_e5m2, b_e5m2, stream) ? launched() : refuse(CKPT_EINVAL, kNoForm);
     if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
     const uint64_t part_bytes = f8_part_bytes(uint64_t(m), uint64_t(n)) * choice.splits;
     if (const char *why = ranges.wrong(workspace, part_bytes)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
@@ -262,7 +264,7 @@ int gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int32_t dtyp
     parts.dtype = CKPT_F32;
     parts.c_split = m * pitch;
     parts.steps_a_split = (steps + choice.splits - 1) / choice.splits;
-    launch_form(choice, parts, wide, a_e5m2, b_e5m2, stream);
+    if (!launch_form(choice, parts, wide, a_e5m2, b_e5m2, stream)) return refuse(CKPT_EINVAL, kNoForm);
     const uint64_t threads = uint64_t(m) * (pitch / 4);
     hipLaunchKernelGGL(f8_join_kernel, dim3(unsigned((threads + 255) / 256)), dim3(256), 0, stream, static_cast<const float *>(workspace), choice.splits, parts.c_split, pitch, p);
     return launched();

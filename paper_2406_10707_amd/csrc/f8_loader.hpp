@@ -29,6 +29,13 @@ struct F8Shape {
     static_assert(!PAIR || TN == 2 * TNG, "a wave has a group of each");
 };
 
+// The product's, in the order of kF8Forms
+template <int FORM> struct F8GemmShape;
+template <> struct F8GemmShape<0> { typedef F8Shape<4, 2, 4, 8, 4, 2, false> type; };
+template <> struct F8GemmShape<1> { typedef F8Shape<4, 2, 4, 4, 4, 3, false> type; };
+template <> struct F8GemmShape<2> { typedef F8Shape<2, 2, 4, 4, 4, 2, false> type; };
+template <> struct F8GemmShape<3> { typedef F8Shape<2, 2, 2, 2, 2, 4, false> type; };
+
 __device__ __forceinline__ uint32_t f8_rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
 
 // Rows past the end of a matrix are its last row again.
