@@ -122,8 +122,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_forward_kernel(GatedForwa
 // Tiles of 256 tokens up to the `whole`th block; behind them each two blocks take the halves of one, where the last round of blocks would leave half of the chip idle: 4096 tokens, 4096 to 11008, 5.4 rounds, 601 -> 569 us; 1024 tokens 204 -> 163.
 template <int ACT, bool SQUARE, int FA>
 __global__ __launch_bounds__(512, 2) void gated_forward_halves_kernel(GatedForward p, TileOrder order, uint32_t whole) {
-    typedef F8Shape<4, 2, 4, 8, 4, 2, true> S;
-    typedef F8Shape<4, 2, 2, 8, 4, 2, true> Half;
+    typedef F8GatedShape<0>::type S;
+    typedef F8GatedShape<1>::type Half;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
     const uint32_t rest = (gridDim.x - whole) / 2, second = blockIdx.x >= whole + rest;
     const GemmTile t = gemm_tile(order, second ? blockIdx.x - rest : blockIdx.x);
@@ -153,10 +153,9 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(GatedForward p, f
 }
 
 // Up to 64 tokens, values in the same rows: tiles of all tokens by 32 columns of gate and of up are four times as many as those with whole blocks of 128 (which of the two: gated_values_first).
-typedef F8Shape<2, 2, 2, 2, 1, 4, true> GatedValuesTile;
 template <int ACT, bool SQUARE, int FA>
 __global__ __launch_bounds__(256, 2) void gated_values_kernel(GatedForward p, float *values, uint64_t pitch) {
-    typedef GatedValuesTile S;
+    typedef F8GatedValuesShape S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
     const int64_t col = int64_t(blockIdx.x) * (S::BN / 2);
@@ -202,7 +201,7 @@ struct GatedBackward {
 // are NaN only where the last row is.
 template <int ACT, bool SQUARE, int FA, bool E5M2>
 __global__ __launch_bounds__(256, 2) void gated_backward_kernel(GatedBackward p, TileOrder order) {
-    typedef F8Shape<2, 2, 4, 4, 4, 2, false> S;
+    typedef F8BackwardShape S;
     // largest magnitudes, [640][2]: 128 rows of dgate, of dup, 128 columns of dgate, of dup, of h, each as two waves have seen it; what they are multiplied with, [640]; gate's and up's codes, [32][256]
     constexpr int DGATE = 0, DUP = 128, DGATE_BY_COL = 256, DUP_BY_COL = 384, H_BY_COL = 512, EVERY = 640;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::BYTES];
@@ -423,9 +422,9 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
             });
             return launched();
         }
-        case 0: return tiles(F8Shape<4, 2, 4, 8, 4, 2, true>());
-        case 1: return tiles(F8Shape<4, 2, 2, 8, 4, 2, true>());
-        default: return tiles(F8Shape<2, 4, 2, 4, 2, 2, true>());
+        case 0: return tiles(F8GatedShape<0>::type());
+        case 1: return tiles(F8GatedShape<1>::type());
+        default: return tiles(F8GatedShape<2>::type());
     }
 }
 

@@ -35,6 +35,13 @@ template <> struct F8GemmShape<0> { typedef F8Shape<4, 2, 4, 8, 4, 2, false> typ
 template <> struct F8GemmShape<1> { typedef F8Shape<4, 2, 4, 4, 4, 3, false> type; };
 template <> struct F8GemmShape<2> { typedef F8Shape<2, 2, 4, 4, 4, 2, false> type; };
 template <> struct F8GemmShape<3> { typedef F8Shape<2, 2, 2, 2, 2, 4, false> type; };
+// Those of the gated block's forward pass, in the order of gated_form; of its values first, and of the backward pass
+template <int FORM> struct F8GatedShape;
+template <> struct F8GatedShape<0> { typedef F8Shape<4, 2, 4, 8, 4, 2, true> type; };
+template <> struct F8GatedShape<1> { typedef F8Shape<4, 2, 2, 8, 4, 2, true> type; };
+template <> struct F8GatedShape<2> { typedef F8Shape<2, 4, 2, 4, 2, 2, true> type; };
+typedef F8Shape<2, 2, 2, 2, 1, 4, true> F8GatedValuesShape;
+typedef F8Shape<2, 2, 4, 4, 4, 2, false> F8BackwardShape;
 
 __device__ __forceinline__ uint32_t f8_rotated(uint32_t three_bits) { return ((three_bits << 1) & 7) | (three_bits >> 2); }
 
