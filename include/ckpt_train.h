@@ -91,7 +91,8 @@ typedef enum { CKPT_F8_E4M3 = 3, CKPT_F8_E5M2 = 4 } ckpt_f8_format;
  * the pitch has beyond is not touched. Half the columns of a wider matrix are such a matrix where they begin at a multiple of 128. Scales
  * lie by blocks of columns, so that a product reads those of neighbouring rows at once: that of element (r, c) is
  * scales[(c / 128) * scale_pitch + r / block_rows], scale_pitch at least ceil(rows / block_rows). What a call writes (codes,
- * scales, plain matrices, workspace) may share no byte with anything else that it reads or writes, and is refused if it does; rows may lie between another's rows. cols is at most 2^23 where a product contracts over them. */
+ * scales, plain matrices, workspace) may share no byte with anything else that it reads or writes, and is refused if it does; rows may lie between another's rows. Where a product or the gated block contracts over a matrix's columns, cols and
+ * code_pitch are at most 2^23. */
 typedef struct {
     int32_t format;        /* ckpt_f8_format */
     int32_t block_rows;    /* 1 or 128 */
@@ -108,7 +109,7 @@ int ckpt_f8_layout(int32_t format, int32_t block_rows, int64_t rows, int64_t col
 
 /* Rounds src, a row-major matrix of src_dtype (CKPT_F32, CKPT_BF16, CKPT_F16; aligned to its element) with `ld` elements from row to row, to by_row (rows x
  * cols) and / or by_col (the transpose: cols x rows), in one pass over src. Either may be NULL; both have the same block_rows, not
- * necessarily the same format unless block_rows is 128. */
+ * necessarily the same format unless block_rows is 128. The conversions take matrices of fewer than 2^24 tiles: of 16 x 512 elements to by_row alone with block_rows 1, of 4 x 512 in ckpt_f8_dequantize, else of 128 x 128. */
 int ckpt_f8_quantize(const void *src, int32_t src_dtype, int64_t ld, const ckpt_f8_matrix *by_row, const ckpt_f8_matrix *by_col, void *stream);
 
 /* The transpose of a matrix that is held in 8 bits: an activation kept by rows from the forward pass, as the product for a weight's gradient contracts over it. With
@@ -140,7 +141,8 @@ typedef enum { CKPT_GATE_SILU = 1, CKPT_GATE_GELU = 2 } ckpt_gate;
 
 /* Both projections, the activation, the product and the rounding to 8 bits in one pass. x is tokens x hidden, w_gate and w_up are ffn x hidden (CKPT_F8_E4M3,
  * blocks of one kind); gate, up and h are tokens x ffn, CKPT_F8_E4M3 with block_rows 1. gate and up are what the backward pass needs, rounded to 8
- * bits (h is made of the values before that rounding); both NULL: nothing is kept, as in serving. Workspace as in ckpt_f8_gemm, for up to 64 tokens. */
+ * bits (h is made of the values before that rounding); both NULL: nothing is kept, as in serving. Workspace as in ckpt_f8_gemm, for up to 64 tokens.
+ * Both passes take fewer than 2^22 tiles: of 256 tokens by 128 columns forward (fewer tokens' tiles are smaller), of 128 by 128 backward. */
 int ckpt_gated_workspace(int64_t tokens, int64_t ffn, int64_t hidden, uint64_t *bytes);
 int ckpt_gated_forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8_matrix *w_up, int32_t activation, const ckpt_f8_matrix *gate,
                        const ckpt_f8_matrix *up, const ckpt_f8_matrix *h, void *workspace, uint64_t workspace_bytes, void *stream);

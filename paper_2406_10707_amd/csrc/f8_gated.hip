@@ -42,7 +42,7 @@ struct GatedForward {
 };
 
 // A tile's columns are 128 of gate and the same 128 of up, in turn groups of 16 TNG, so that a lane has both factors of its elements. The rows' largest values of 128 columns are found among the lanes of a row (q), then
-// through LDS among the WN waves. 4096 tokens, 4096 to 11008, all three matrices kept, 570 to 625 us from card to card (1.2 to 1.3 PFLOP/s): the sums (f8_tile.hpp), and some 30 us of rounds' ends.
+// through LDS among the WN waves. 4096 tokens, 4096 to 11008, all three matrices kept, 569 to 625 us from card to card in a row of calls (1.2 to 1.3 PFLOP/s; a trace's first ones up to 690): the sums (f8_tile.hpp), and some 30 us of rounds' ends.
 template <class S, int ACT, bool SQUARE, int FA>
 __device__ __forceinline__ void gated_forward_tile(const GatedForward &p, uint8_t *lds, int64_t row, int64_t col) {
     static_assert(S::PAIR && S::BN == 256, "a tile has a block of each");
@@ -347,9 +347,9 @@ void with_kinds(int32_t activation, bool e5m2, bool square, F f) {
     else with_format(std::integral_constant<int, CKPT_GATE_GELU>());
 }
 
-// Sides are at most 2^31 - 1; the product of tiles is at most 2^24 - 1, so that a grid has fewer than 2^32 work-items.
+// Sides are at most 2^31 - 1. Fewer than 2^22 tiles, of up to 512 threads (and half a round of halves): a grid has fewer than 2^32 work-items.
 bool fits_grid(int64_t down, int64_t across) { return down * across < 1 << 22; }
-constexpr const char *kTooManyTiles = "more than 2^22 tiles of tokens and columns";
+constexpr const char *kTooManyTiles = "2^22 tiles of tokens and columns or more";
 
 // What the values of few tokens take, 0 where they are rounded in one launch.
 uint64_t values_pitch(int64_t ffn) { return f8_padded(ffn); }

@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256) void f8_values_kernel(F8Held from, uint8_t *ds
 
 // ------------------------------------------------------------------ host
 
-constexpr const char *kTooLarge = "the matrix takes more than 2^24 blocks of threads";
+constexpr const char *kTooLarge = "the matrix takes 2^24 blocks of threads or more";
 bool fits_grid(uint64_t down, uint64_t across) { return down < 1u << 24 && across < 1u << 24 && down * across < 1u << 24; }
 
 template <int SRC>

@@ -13,7 +13,8 @@
 //
 // Measured, 8192 x 8192 x 8192: 463 us in 8 bits (2.37 PFLOP/s; at 2.0 GHz, 57 % of the matrix instructions' cycles at 4096 x 4096 x 11008), 865 us in bf16 (1.27 PFLOP/s; a plain bf16 product of that size by the image's library 776). What bounds both is the
 // vector instructions beside the matrix instructions, and power. In bf16 a step of a 64 x 64 wave has 64 matrix instructions, 128 conversions, 64 multiply-adds and, with scales of single rows of B, 64 products of scales: 11008 x 4096 x 8192 added to f32 705 to
-// 740 us, at 1.9 GHz, where the matrix instructions take 47 % of a SIMD's cycles and the vector instructions (4.9 cycles a conversion, 2.7 a multiply-add) about as many. Larger waves convert less but do not fit the registers; the same loop without conversions and multiply-adds runs at 1.6 PFLOP/s.
+// 740 us, at 1.9 GHz, where the matrix instructions take 47 % of a SIMD's cycles and the vector instructions (4.9 cycles a conversion, 2.7 a multiply-add) about as many. Waves of 64 x 128 (256 x 256 tiles) have a quarter fewer conversions
+// to a matrix instruction, spill two to nine registers, and cost 2 % less a step, so that conversions alone are not it; the same loop without conversions and multiply-adds runs at 1.6 PFLOP/s.
 #pragma once
 #include <type_traits>
 
@@ -296,7 +297,7 @@ __device__ __forceinline__ void f8_sums(f32x4 (&acc)[S::TM][S::TN], uint8_t *lds
 
 // As single tokens give them: B is what has to be read, once, at the rate of memory. A block takes 16 rows of B (of each of MATRICES); its waves take the windows of four steps in turn, each with LDS of its own, so that none waits
 // for another before the sums are added, in wave order. Four steps of B and A are under way a wave; a step's place is filled again as soon as it has been read. One row through 4096 x 11008 10 us from memory that the last level of cache
-// holds in part, 12.8 from HBM (3.5 TB/s: a launch, then five or six windows of a wave in a row), through 28672 x 8192 42 (5.6 TB/s).
+// holds in part, 12.8 from HBM (3.5 TB/s), through 28672 x 8192 42 (5.6 TB/s). What the former waits for is not known: eight waves, with twice as much under way, take 13.0.
 template <int WAVES, int MATRICES, bool EIGHT>
 struct F8Few {
     typedef F8FewLoader<MATRICES, EIGHT> Loader;

@@ -1,4 +1,4 @@
-"""A small training run with everything include/ckpt_train.h has, next to what the library is for: two linear layers trained on a fixed linear target in 4-bit products with 8-bit moments,
+"""A small training run with the optimizer and the 4-bit operators of include/ckpt_train.h, next to what the library is for: two linear layers trained on a fixed linear target in 4-bit products with 8-bit moments,
 snapshots while it goes on, and a restart from the first of them that ends in the same bits.
 
     python -m paper_2406_10707_amd.train_example [--steps 60] [--every 20] [--dir /dev/shm/...]
