@@ -136,7 +136,8 @@ int ckpt_f8_gemm(const ckpt_f8_matrix *a, const ckpt_f8_matrix *b, void *c, int3
  *
  * h = act(x Wg^T) * (x Wu^T), y = h Wd^T: the last is ckpt_f8_gemm. Activations:
  *   CKPT_GATE_SILU  act(g) = g / (1 + exp(-g))
- *   CKPT_GATE_GELU  act(g) = g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
+ *   CKPT_GATE_GELU  act(g) = g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)))
+ * Where the factor of g, 1 / (1 + exp(-g)) or half of 1 + tanh, is below 2^-126, it may count as zero, and act and its slope with it. */
 typedef enum { CKPT_GATE_SILU = 1, CKPT_GATE_GELU = 2 } ckpt_gate;
 
 /* Both projections, the activation, the product and the rounding to 8 bits in one pass. x is tokens x hidden, w_gate and w_up are ffn x hidden (CKPT_F8_E4M3,
