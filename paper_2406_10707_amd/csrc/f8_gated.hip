@@ -390,7 +390,7 @@ int forward(const ckpt_f8_matrix *x, const ckpt_f8_matrix *w_gate, const ckpt_f8
         if (uint64_t(workspace) % 16) return refuse(CKPT_EINVAL, "workspace must be 16-byte aligned");
         if (const char *why = ranges.wrong(workspace, bytes)) return refuse(CKPT_EINVAL, std::string("workspace: ") + why);
         for (const auto &e : every)
-            if (e.m && overlap(*e.m, Rows{uint64_t(workspace), bytes, bytes, 1})) return refuse(CKPT_EINVAL, std::string("workspace: overlaps ") + e.name);
+            if (e.m && overlap(*e.m, Rows{uint64_t(workspace), bytes, bytes, 1})) return refuse(CKPT_EINVAL, std::string(e.name) + "overlaps the workspace");
         float *values = static_cast<float *>(workspace);
         const uint64_t pitch = values_pitch(ffn);
         if (uint64_t(tokens) > kF8Few)
